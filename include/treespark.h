@@ -338,6 +338,94 @@ int32_t ts_calib_refit(ts_ctx* ctx, const uint64_t* stats, int32_t population, i
 int32_t ts_calib_load_table(ts_ctx* ctx, const float* table, void* stream);
 
 /*
+ * The cache in which the target keeps its keys and values, in 4 bits, and the calls around it.  (The paper's engine keeps a
+ * row of a preallocated buffer per request and a valid set, Section 4; the layout below is this library's own.)  A round of a
+ * caller that uses it: ts_cache_reserve, per layer ts_cache_append and ts_tree_attention, after ts_verify_tree
+ * ts_cache_commit.
+ *
+ * Tokens of a request stand in pages; row b of the block table [B][max_pages] holds the page of tokens 0..page_size-1, of the
+ * next page_size tokens, and so on.  seq_len[b] tokens are committed (the prefix); a round's rows are the anchor and the
+ * n_nodes[b] nodes of the request's tree and stand at positions seq_len[b] .. seq_len[b] + n_nodes[b].  A slot = page *
+ * page_size + place in the page.  Row arrays are [B][Nmax+1] as ts_emit_attention_inputs lays them out; where n_nodes is
+ * NULL a request has its anchor only and row arrays are [B][1] (one token per request and round).  n_nodes is clamped to
+ * 0..Nmax.  seq_len[b] < 0: the request takes no part.
+ *
+ * Layout of one layer's pool, bytes: [n_pages][Hkv][page_size / 16][18 * Dh].  The 18 * Dh bytes of 16 consecutive tokens of
+ * a head are K codes [16][Dh/2], V codes [2][Dh/16][8][8], K scales [16][Dh/16], V scales [2][Dh/16][8] (V: octets of
+ * tokens, groups of 16 channels, tokens of the octet).  A code c in 0..15 and the e4m3 scale s of its 16 channels stand for
+ * (c - 8) * s * 2^exp, exp = k_exp or v_exp.  Eight channels share a 32-bit word: channel 2j is nibble j, channel 2j + 1
+ * nibble j + 4.
+ */
+typedef struct {
+  int32_t Hq, Hkv, Dh;                   /* query heads (a multiple of Hkv, at most 1024), key/value heads, channels: 64 or 128 */
+  int32_t page_size, n_pages, max_pages; /* tokens of a page (a multiple of 16, at most 4096), pages, columns of the table */
+  int32_t dtype;                         /* TS_DTYPE_* of q, k, v and the results */
+  int32_t k_exp, v_exp;                  /* powers of two of the scales, -30..30; 0 fits keys and values of ordinary size */
+} ts_cache_layout;
+
+/* Bytes of one layer's pool; 0 for a layout that is not supported. */
+size_t ts_cache_bytes(const ts_cache_layout* layout);
+
+/*
+ * Pages and slots for a round.  Request b needs ceil((seq_len + rows) / page_size) pages and has held[b]; what is missing is
+ * taken from the end of free_pages [n_pages] (free_count[0] entries), the first request first: the k-th page taken is
+ * free_pages[free_count - 1 - k].  New table entries held[b] .. are written, others are left as they are.  A request whose
+ * pages would pass the list's beginning, or that needs more than max_pages, is refused: status TS_ERR_OVERFLOW, no slots,
+ * nothing taken; so are all later ones that need pages (those that need none are served).
+ * seq_len[b] < 0: the request's pages go back to the list, its table entries become -1, held 0.  They can be taken by the
+ * next call.
+ *   slot_map [B][Nmax+1] ([B][1]): slot of each row, -1 for unused rows, refused requests and entries that are no page.
+ *   held_out [B], free_count_out [1]: the new counts; may be the arrays held and free_count themselves.
+ *   status [B]: TS_OK or TS_ERR_OVERFLOW.
+ * All DEVICE int32; other arrays must not overlap.
+ */
+int32_t ts_cache_reserve(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B, const int32_t* seq_len, const int32_t* n_nodes,
+                         const int32_t* held, int32_t* free_pages, const int32_t* free_count, int32_t* block_table,
+                         int32_t* held_out, int32_t* free_count_out, int32_t* slot_map, int32_t* status, void* stream);
+
+/*
+ * Write keys and values of `rows` rows to their slots.  k, v: [rows][Hkv][Dh] with ldk, ldv elements between rows (so that
+ * slices of one projection can be passed); slot_map DEVICE [rows], entries outside the pool are skipped; a slot that occurs
+ * twice gets one of the two in part or whole.  The scale of 16 channels is max|x| 2^-exp / 7 rounded to e4m3 (nearest even,
+ * at most 448), a code rint(x 2^-exp / scale) within -8..7 (0 where the scale is 0).  A row whose keys or values of a head
+ * are not all finite (after the multiplication with 2^-exp) has NaN scales for that head, K and V: every query that attends
+ * to it gets NaN.
+ *   k_val, v_val: DEVICE [rows][Hkv][Dh] contiguous, or NULL: what the cache holds now, for a caller that wants to compute
+ *   with the same values.  Rows without a slot are left as they were.
+ */
+int32_t ts_cache_append(ts_ctx* ctx, const ts_cache_layout* layout, int32_t rows, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                        const int32_t* slot_map, void* pool, void* k_val, void* v_val, void* stream);
+
+/*
+ * Attention of a round's rows over the cache (Section 3.2 item 3: row i attends to the prefix and to its root path).
+ *   out[b][i][hq] = sum_j softmax_j(scale * q[b][i][hq] . K_j) V_j,  kv head = hq / (Hq / Hkv), over
+ *     the prefix, the anchor, and the nodes whose bits are set in mask[b][i-1] (ts_expand_tree's ancestor bitmask, which has
+ *     the node's own bit); the anchor's row sees no node.  mask NULL: a chain or a prompt's chunk, row i sees rows 0..i.
+ *   lse [B][rows][Hq] or NULL: natural logarithm of the sum of exponentials (two contexts' results can be joined by it).
+ * q and out: [B][Nmax+1][Hq][Dh] ([B][Hq][Dh] without n_nodes) with ldq, ldo elements between rows; the rows of this round
+ * have been appended.  Unused rows and requests with seq_len < 0 are left as they were.  Tokens whose table entry is no
+ * page are absent; a row that sees no token gets 0 and lse = -inf.  What stands in the cache behind the last row, or in
+ * nodes that a row does not see, does not matter, NaN included.  ws: ts_tree_attention_workspace_bytes() bytes (it does not
+ * grow with B or the lengths); calls that overlap on the GPU, replayed graphs among them, need one each.  A bounded
+ * device-side wait that runs out gives NaN.
+ */
+size_t ts_tree_attention_workspace_bytes(const ts_ctx* ctx, const ts_cache_layout* layout, int32_t B);
+int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B, const void* q, int64_t ldq, const void* pool,
+                          const int32_t* block_table, const int32_t* seq_len, const int32_t* n_nodes, const uint64_t* mask,
+                          float scale, void* out, int64_t ldo, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Keep the accepted path: for i < acc_len[b] the keys and values of row 1 + acc_node[b][i] move to row 1 + i, in all layers
+ * (pool of layer l = pool + l * layer_stride bytes); all sources of a request are read before its targets are written.
+ * seq_len_out[b] = seq_len[b] + 1 + acc_len[b] (the anchor's row is in its place; may be seq_len itself); the bonus token is
+ * the next round's anchor.  acc_len [B], acc_node [B][D] as written by ts_verify_tree.  Moves whose node lies outside
+ * 0..Nmax-1 or whose slot has no page are skipped.  Pages stay held.  seq_len[b] < 0: nothing happens.
+ */
+int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B, int32_t layers, size_t layer_stride, void* pool,
+                        const int32_t* block_table, const int32_t* seq_len, const int32_t* acc_len, const int32_t* acc_node,
+                        int32_t* seq_len_out, void* stream);
+
+/*
  * Instrumentation (no counterpart in the paper): per-kernel device times and launch counts.
  * ts_profile_enable(capacity > 0) creates `capacity` CUDA event pairs and from then on every kernel
  * the hot calls launch is bracketed by an event pair on the caller's stream until the pairs run out;

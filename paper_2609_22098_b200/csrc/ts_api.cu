@@ -125,6 +125,7 @@ extern "C" int32_t ts_create(const ts_config* cfg, ts_ctx** out) {
   if (e == cudaSuccess) e = verify_setup(ctx);
   if (e == cudaSuccess) e = walk_setup(ctx);
   if (e == cudaSuccess) e = expand_setup(ctx);
+  if (e == cudaSuccess) e = attn_setup(ctx);
   if (e != cudaSuccess) { cudaFree(ctx->d_table); delete (Prof*)ctx->prof; delete ctx; return set_cuda_error("ts_create", e); }
   *out = ctx;
   return TS_OK;
@@ -169,7 +170,7 @@ extern "C" size_t ts_workspace_bytes(const ts_ctx* ctx, int32_t batch) {
 
 static const char* kKernelNames[K_COUNT] = {"expand_init", "score_tile", "score_merge", "expand_level", "expand_finalize",
                                             "zrow_stats", "verify_greedy", "verify_walk", "score_few", "allocate_select", "allocate_cut",
-                                            "calib_accumulate", "calib_refit", "attention_inputs", "expand_persistent"};
+                                            "calib_accumulate", "calib_refit", "attention_inputs", "expand_persistent", "cache_reserve", "cache_append", "cache_commit", "attention_few", "attention_join"};
 
 extern "C" const char* ts_kernel_name(int32_t id) { return (id >= 0 && id < K_COUNT) ? kKernelNames[id] : nullptr; }
 

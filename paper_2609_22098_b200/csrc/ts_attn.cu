@@ -1,0 +1,511 @@
+// Attention of a round's rows over the 4-bit cache: the entry point, the kernel for few query rows a kv head, and the kernel
+// that joins the pieces of cut units.
+#include "ts_attn.cuh"
+#include "ts_tc.cuh"
+
+namespace ts {
+
+// ------------------------------------------------------------------------------------------------
+// Few rows: 8 NT query rows of one kv head a unit, on mma.sync with the cache's tokens on the rows of the matrix
+// instruction (S^T = K Q^T, O^T = V^T P^T), so that one instruction of 16 x 8 serves eight query rows and no lane computes
+// for rows that are not there.
+// ------------------------------------------------------------------------------------------------
+constexpr int FEW_WARPS = 4;
+constexpr int FEW_THREADS = FEW_WARPS * 32;
+
+template <int Dh, int NT>
+struct FewPlan {
+  static constexpr int QT = 8 * NT;
+  static constexpr int BLK = cache_block_bytes(Dh);
+  static constexpr int STAGES = 4;
+  static constexpr int ROW = Dh + 4;                       // floats between rows of the merge buffer
+  static constexpr int RING = FEW_WARPS * STAGES * BLK;
+  static constexpr int MERGE = FEW_WARPS * QT * (ROW + 2) * 4;
+  static constexpr int SMEM = RING + MERGE;
+};
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+// The query rows of a unit as B operands: lane (g, t) holds channels t Dh/4 .. of row g of each tile of eight.  A row is
+// multiplied by the power of two that brings its largest element to 2^14..2^15: bf16 then is exact in fp16 down to 2^-38 of
+// that element.  fp32 is split into two fp16 parts, exact to 2^-22.  f: what a column's scores are multiplied with.
+template <int Dh, int NT, bool F32>
+struct Queries {
+  static constexpr int REGS = Dh / 8;   // registers a tile
+  uint32_t hi[NT][REGS];
+  uint32_t lo[F32 ? NT : 1][F32 ? REGS : 1];
+  float f[NT][2];
+
+  __device__ __forceinline__ void load(const AttnArgs& a, const AttnUnit& u, int h, int first, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int idx = first + 8 * n + g;
+      float x[Dh / 4];
+      if (idx < u.rows * a.d.G) {
+        const size_t at = ((size_t)u.b * a.rcap + idx / a.d.G) * a.ldq + (size_t)(h * a.d.G + idx % a.d.G) * Dh + t * (Dh / 4);
+        if (F32) {
+          const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + at);
+#pragma unroll
+          for (int i = 0; i < Dh / 16; ++i) {
+            const float4 v = __ldg(p + i);
+            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+          }
+        } else {
+          const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + at);
+#pragma unroll
+          for (int i = 0; i < Dh / 32; ++i) unpack_bf16x8(__ldg(p + i), x + 8 * i);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < Dh / 4; ++i) x[i] = 0.f;
+      }
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < Dh / 4; ++i) top = fmaxf(top, fabsf(x[i]));
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+      const int e = max((int)(__float_as_uint(top) >> 23), 20);         // biased exponent; 2^(141 - e) has to be a float
+      const float up = __uint_as_float((unsigned)(127 + 141 - e) << 23), mine = a.qk * __uint_as_float((unsigned)(127 + e - 141) << 23);
+#pragma unroll
+      for (int i = 0; i < REGS; ++i) {
+        const float x0 = x[2 * i] * up, x1 = x[2 * i + 1] * up;
+        const __half2 v = __floats2half2_rn(x0, x1);
+        hi[n][i] = as_u32(v);
+        if (F32) lo[n][i] = as_u32(__floats2half2_rn(x0 - __low2float(v), x1 - __high2float(v)));
+      }
+      f[n][0] = __shfl_sync(~0u, mine, 8 * t);
+      f[n][1] = __shfl_sync(~0u, mine, 8 * t + 4);
+    }
+  }
+};
+
+template <int Dh, int NT, bool F32>
+__global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_kernel(const AttnArgs a) {
+  using P = FewPlan<Dh, NT>;
+  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+  constexpr int QT = P::QT, ST = P::STAGES, BLK = P::BLK;
+  constexpr int MT = Dh / 16;        // tiles of 16 channels
+  constexpr int KW = Dh / 32;        // words of a token's K codes that a lane holds
+  constexpr float ROOM = F32 ? 0.f : 8.f, LIFT = F32 ? 15.f : 7.f;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ uint64_t bars[FEW_WARPS][ST];
+  __shared__ int present[FEW_WARPS][ST];
+  __shared__ int gave_up;
+  float* merge = reinterpret_cast<float*>(smem + P::RING);
+  float* merge_ml = merge + FEW_WARPS * QT * P::ROW;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  if (threadIdx.x == 0) gave_up = 0;
+  if (lane == 0) {
+#pragma unroll
+    for (int s = 0; s < ST; ++s) mbar_init(&bars[w][s], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  AttnUnit u;
+  long long start, end;
+  int active;
+  if (!attn_locate<FEW_THREADS>(a, QT, u, start, end, active)) return;
+
+  // The copies run ahead of the arithmetic, across units: cursor and page of the block to fetch next.
+  unsigned char* ring = smem + w * ST * BLK;
+  AttnUnit fu = u;
+  long long fp = start + w;
+  int fpage = -1, finner = 0, fslot = 0;
+  const int per = a.d.ps / CACHE_BLOCK;
+  auto look_up = [&]() {
+    if (fp >= end) return;
+    while (fp >= fu.t0 + fu.nblk) next_unit(a, QT, fu);
+    const int j = (int)(fp - fu.t0), c = j / per;
+    finner = j - c * per;
+    fpage = c < a.d.cols ? __ldg(a.table + (size_t)fu.b * a.d.cols + c) : -1;
+  };
+  auto fetch = [&]() {
+    if (fp < end) {
+      if (lane == 0) {
+        const long long off = block_offset(a.d, fpage, finner, fu.v / fu.nq);
+        present[w][fslot] = off >= 0;
+        if (off >= 0) {
+          mbar_expect_tx(&bars[w][fslot], BLK);
+          bulk_load(ring + fslot * BLK, a.pool + off, BLK, &bars[w][fslot]);
+        } else mbar_arrive(&bars[w][fslot]);
+      }
+      fp += FEW_WARPS;
+      if (++fslot == ST) fslot = 0;
+      look_up();
+    }
+  };
+  look_up();
+#pragma unroll
+  for (int s = 0; s < ST; ++s) fetch();
+
+  int slot = 0;
+  uint32_t phase = 0;
+  long long pos = start, p = start + w;
+  while (pos < end) {
+    const int h = u.v / u.nq, first = (u.v - h * u.nq) * QT;
+    const long long t1 = u.t0 + u.nblk, seg_end = min(t1, end);
+    Queries<Dh, NT, F32> q;
+    q.load(a, u, h, first, lane);
+    float o[NT][MT][4], m[NT][2], ref[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[n][i][c] = 0.f;
+      m[n][0] = m[n][1] = -INFINITY; ref[n][0] = ref[n][1] = 0.f; l[n][0] = l[n][1] = 0.f;
+    }
+    for (; p < seg_end; p += FEW_WARPS) {
+      const bool ok = mbar_wait(&bars[w][slot], phase, (volatile int*)&gave_up, nullptr, a.limit);
+      const bool here = present[w][slot] != 0;
+      const unsigned char* blk = ring + slot * BLK;
+      // ---- scores of 16 tokens: s[n] = rows g, g + 8 (tokens), columns 2t, 2t + 1 (queries)
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+      {
+        uint32_t kw[2][KW];
+        __half2 sc[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const unsigned char* row = blk + (g + 8 * e) * (Dh / 2) + t * (Dh / 8);
+          if (Dh == 128) {
+            const uint4 v = *reinterpret_cast<const uint4*>(row);
+            kw[e][0] = v.x; kw[e][1] = v.y; kw[e][KW - 2] = v.z; kw[e][KW - 1] = v.w;
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(row);
+            kw[e][0] = v.x; kw[e][1] = v.y;
+          }
+          const unsigned char* sp = blk + off_ks(Dh) + (g + 8 * e) * (Dh / CACHE_GROUP) + t * (Dh / 64);
+          sc[e] = k_scales(Dh == 128 ? *reinterpret_cast<const unsigned short*>(sp) : *sp);
+        }
+#pragma unroll
+        for (int i = 0; i < KW; ++i) {
+          uint32_t x[2][4];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const __half2 ss = Dh == 128 && i >= KW / 2 ? __high2half2(sc[e]) : __low2half2(sc[e]);
+            unpack8(kw[e][i], ss, __hmul2(ss, __float2half2_rn(-1032.f)), __hmul2(ss, __float2half2_rn(-72.f)), x[e]);
+          }
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const uint32_t fr[4] = {x[0][2 * v], x[1][2 * v], x[0][2 * v + 1], x[1][2 * v + 1]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const int r = 4 * i + 2 * v;
+              if (F32) {
+                // each step's sum apart and added in fp32: the instruction's own accumulation rounds towards zero
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_16816(c, fr, q.lo[F32 ? n : 0][F32 ? r : 0], q.lo[F32 ? n : 0][F32 ? r + 1 : 0]);
+                mma_16816(c, fr, q.hi[n][r], q.hi[n][r + 1]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[n][k] += c[k];
+              } else {
+                mma_16816(s[n], fr, q.hi[n][r], q.hi[n][r + 1]);
+              }
+            }
+          }
+        }
+      }
+      // ---- weights
+      const int tok0 = (int)(p - u.t0) * CACHE_BLOCK;
+      const bool masked = tok0 > u.seq - CACHE_BLOCK || !here || !ok;
+      uint32_t ph[NT][2], pl[F32 ? NT : 1][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[n][c] *= q.f[n][c & 1];
+        if (masked) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int rel = tok0 + g + 8 * (c >> 1) - u.seq, idx = first + 8 * n + 2 * t + (c & 1);
+            const bool sees = here && (rel < 0 || row_sees(a, u.b, idx / a.d.G, rel, u.rows));
+            if (!sees) s[n][c] = -INFINITY;
+            if (!ok) s[n][c] = NAN;
+          }
+        }
+        // The reference of the exponents moves only when a score passes it by more than ROOM: weights stay below
+        // 2^(ROOM + LIFT) = 2^15, and LIFT keeps small ones out of fp16's subnormals.
+        const bool up = fmaxf(s[n][0], s[n][2]) > m[n][0] || fmaxf(s[n][1], s[n][3]) > m[n][1];
+        if (__any_sync(~0u, up)) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float top = fmaxf(s[n][c], s[n][c + 2]);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+            if (top > m[n][c]) {
+              const float r = m[n][c] == -INFINITY ? 0.f : ex2(ref[n][c] - (top - LIFT));
+              m[n][c] = top + ROOM; ref[n][c] = top - LIFT;
+              l[n][c] *= r;
+#pragma unroll
+              for (int i = 0; i < MT; ++i) { o[n][i][c] *= r; o[n][i][c + 2] *= r; }
+            }
+          }
+        }
+        float e[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) e[c] = ex2(s[n][c] - ref[n][c & 1]);
+        l[n][0] += e[0] + e[2]; l[n][1] += e[1] + e[3];
+        const __half2 h0 = __floats2half2_rn(e[0], e[1]), h1 = __floats2half2_rn(e[2], e[3]);
+        ph[n][0] = transpose8(as_u32(h0)); ph[n][1] = transpose8(as_u32(h1));
+        if (F32) {
+          pl[F32 ? n : 0][0] = transpose8(as_u32(__floats2half2_rn(e[0] - __low2float(h0), e[1] - __high2float(h0))));
+          pl[F32 ? n : 0][1] = transpose8(as_u32(__floats2half2_rn(e[2] - __low2float(h1), e[3] - __high2float(h1))));
+        }
+      }
+      // ---- O^T += V^T P^T: lane (g, t) holds Dh/8 channels of tokens 2t, 2t + 1 of both octets
+      {
+        constexpr int VW = Dh / 64;   // words of a token that a lane holds
+        uint32_t va[2][VW], vb[2][VW];
+        __half2 vs[2], c1032[2], c72[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const unsigned char* oct = blk + off_vc(Dh) + e * (4 * Dh);
+          if (Dh == 128) {
+            const uint4 v = *reinterpret_cast<const uint4*>(oct + g * 64 + t * 16);
+            va[e][0] = v.x; va[e][VW - 1] = v.y; vb[e][0] = v.z; vb[e][VW - 1] = v.w;
+          } else {
+            va[e][0] = *reinterpret_cast<const uint32_t*>(oct + (g >> 1) * 64 + t * 16 + (g & 1) * 4);
+            vb[e][0] = *reinterpret_cast<const uint32_t*>(oct + (g >> 1) * 64 + t * 16 + 8 + (g & 1) * 4);
+          }
+          vs[e] = v_scales(*reinterpret_cast<const unsigned short*>(blk + off_vs(Dh) + e * (Dh / 2) + (Dh == 128 ? g : g >> 1) * 8 + 2 * t));
+          c1032[e] = __hmul2(vs[e], __float2half2_rn(-1032.f));
+          c72[e] = __hmul2(vs[e], __float2half2_rn(-72.f));
+        }
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+          uint32_t lo[2][4], hi[2][4];   // even and odd channels of the word, tokens in the halves
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            unpack8(__byte_perm(va[e][i], vb[e][i], 0x5410), vs[e], c1032[e], c72[e], lo[e]);
+            unpack8(__byte_perm(va[e][i], vb[e][i], 0x7632), vs[e], c1032[e], c72[e], hi[e]);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t fr[4] = {lo[0][j], hi[0][j], lo[1][j], hi[1][j]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float* acc = o[n][4 * i + j];
+              if (F32) {
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_16816(c, fr, pl[F32 ? n : 0][0], pl[F32 ? n : 0][1]);
+                mma_16816(c, fr, ph[n][0], ph[n][1]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[k] += c[k];
+              } else {
+                mma_16816(acc, fr, ph[n][0], ph[n][1]);
+              }
+            }
+          }
+        }
+      }
+      __syncwarp();   // every lane has read the slot that the next copy goes to
+      if (++slot == ST) { slot = 0; phase ^= 1u; }
+      fetch();
+    }
+    // ---- the four warps' parts of the unit
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float sum = l[n][c];
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) sum += __shfl_xor_sync(~0u, sum, x);
+        const int row = w * QT + 8 * n + 2 * t + c;
+        if (g == 0) { merge_ml[2 * row] = m[n][c] == -INFINITY ? -INFINITY : ref[n][c]; merge_ml[2 * row + 1] = sum; }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) *reinterpret_cast<float2*>(merge + row * P::ROW + g * (Dh / 8) + 2 * i) = make_float2(o[n][i][c], o[n][i][c + 2]);
+      }
+    __syncthreads();
+    const bool whole = pos == u.t0 && seg_end == t1;
+    const size_t piece = ((size_t)blockIdx.x * 2 + (start > u.t0 ? 0 : 1)) * QT;
+    for (int e = threadIdx.x; e < QT * Dh; e += FEW_THREADS) {
+      const int row = e / Dh, ch = e - row * Dh, idx = first + row;
+      if (idx >= u.rows * a.d.G) continue;
+      float top = -INFINITY, wm[FEW_WARPS], sum = 0.f, x = 0.f;
+#pragma unroll
+      for (int k = 0; k < FEW_WARPS; ++k) top = fmaxf(top, wm[k] = merge_ml[2 * (k * QT + row)]);
+#pragma unroll
+      for (int k = 0; k < FEW_WARPS; ++k) {
+        const float r = part_weight(wm[k], top);
+        sum += r * merge_ml[2 * (k * QT + row) + 1];
+        x += r * merge[(k * QT + row) * P::ROW + ch];
+      }
+      if (whole) {
+        store_out(reinterpret_cast<T*>(a.out) + out_row(a, u.b, h, idx) + ch, x * row_inv(sum) * a.vo);
+        if (ch == 0 && a.lse) a.lse[lse_row(a, u.b, h, idx)] = row_lse(top, sum);
+      } else {
+        a.part[(piece + row) * Dh + ch] = x;
+        if (ch == 0) { a.part_ml[2 * (piece + row)] = top; a.part_ml[2 * (piece + row) + 1] = sum; }
+      }
+    }
+    __syncthreads();
+    pos = seg_end;
+    if (pos < end) next_unit(a, QT, u);
+  }
+  // after a wait that gave up copies may still be on their way into this CTA's memory
+  if (gave_up)
+    for (int s = 0; s < ST; ++s) {
+      const int n = (int)(((fp - start - w) / FEW_WARPS + ST - 1 - s) / ST);   // copies that went to the slot
+      for (uint32_t i = 0; n > 0 && i < a.limit && !mbar_try_wait(&bars[w][s], (n - 1) & 1); ++i) __nanosleep(100);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Join: one CTA a (cut unit, query row).  The pieces are added in their order, so results do not depend on timing.
+// ------------------------------------------------------------------------------------------------
+constexpr int JOIN_WARPS = 4;
+
+template <int Dh, typename T>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnArgs a, int QT) {
+  constexpr int V = Dh / 32;
+  __shared__ float acc[JOIN_WARPS][Dh], red[JOIN_WARPS][2];
+  pdl_wait();
+  pdl_launch_dependents();
+  const AttnRecord r = a.records[blockIdx.x];
+  if (r.first < 0) return;
+  const int h = r.v / r.nq, row = blockIdx.y, idx = (r.v - h * r.nq) * QT + row;
+  if (idx >= request_rows(a.n_nodes, r.b, a.rcap) * a.d.G) return;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = r.last - r.first + 1;
+  // piece k: the first begins at or before the unit and is its CTA's last; the others begin within it
+  auto at = [&](int k) { return ((size_t)(r.first + k) * 2 + (k == 0 ? 1 : 0)) * QT + row; };
+  float top = -INFINITY;
+  for (int k = threadIdx.x; k < n; k += JOIN_WARPS * 32) top = fmaxf(top, a.part_ml[2 * at(k)]);
+#pragma unroll
+  for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+  if (lane == 0) red[w][0] = top;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < JOIN_WARPS; ++k) top = fmaxf(top, red[k][0]);
+  float sum = 0.f, x[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = 0.f;
+#pragma unroll 4
+  for (int k = w; k < n; k += JOIN_WARPS) {
+    const float wgt = part_weight(a.part_ml[2 * at(k)], top);
+    sum += wgt * a.part_ml[2 * at(k) + 1];
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] += wgt * a.part[at(k) * Dh + lane + 32 * i];
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[w][lane + 32 * i] = x[i];
+  if (lane == 0) red[w][1] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < JOIN_WARPS; ++k) sum += red[k][1];
+  for (int ch = threadIdx.x; ch < Dh; ch += JOIN_WARPS * 32) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < JOIN_WARPS; ++k) v += acc[k][ch];
+    store_out(reinterpret_cast<T*>(a.out) + out_row(a, r.b, h, idx) + ch, v * row_inv(sum) * a.vo);
+  }
+  if (threadIdx.x == 0 && a.lse) a.lse[lse_row(a, r.b, h, idx)] = row_lse(top, sum);
+}
+
+static size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+static size_t attn_workspace(int grid, int QT, int Dh) {
+  return round256((size_t)grid * sizeof(AttnRecord)) + round256((size_t)grid * 2 * QT * Dh * 4) + round256((size_t)grid * 2 * QT * 2 * 4);
+}
+
+static void attn_place(AttnArgs& a, int QT, char* ws) {
+  a.records = (AttnRecord*)ws;
+  a.part = (float*)(ws + round256((size_t)a.grid * sizeof(AttnRecord)));
+  a.part_ml = (float*)((char*)a.part + round256((size_t)a.grid * 2 * QT * a.d.Dh * 4));
+}
+
+// Query rows of a unit and CTAs of a launch.
+static int few_tiles_of(const CacheDims& d, int rcap, bool f32) { return !f32 && (long long)rcap * d.G > 8 ? 2 : 1; }
+static int few_ctas(int nt, bool f32) { return f32 || nt > 1 ? 2 : 3; }
+
+size_t attn_few_workspace(const ts_ctx* ctx, const CacheDims& d, bool f32) {
+  size_t most = 0;
+  for (int nt = 1; nt <= 2; ++nt) {
+    const size_t n = attn_workspace(ctx->num_sms * few_ctas(nt, f32), 8 * nt, d.Dh);
+    most = n > most ? n : most;
+  }
+  return most;
+}
+
+template <int Dh, int NT, bool F32>
+static cudaError_t launch_few(ts_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
+  using P = FewPlan<Dh, NT>;
+  cudaError_t e;
+  {
+    ProfScope ps(ctx, K_ATTN_FEW, st);
+    e = launch_kernel(attn_few_kernel<Dh, NT, F32>, dim3(a.grid), dim3(FEW_THREADS), P::SMEM, st, true, a);
+  }
+  if (e != cudaSuccess) return e;
+  ProfScope ps(ctx, K_ATTN_JOIN, st);
+  return launch_kernel(attn_join_kernel<Dh, typename std::conditional<F32, float, __nv_bfloat16>::type>, dim3(a.grid, P::QT), dim3(JOIN_WARPS * 32), 0, st, true, a, P::QT);
+}
+
+cudaError_t attn_setup(ts_ctx* ctx) {
+  cudaError_t e = cudaSuccess;
+  auto allow = [&](auto kernel) { if (e == cudaSuccess) e = allow_all_smem(kernel, ctx->max_smem); };
+  allow(attn_few_kernel<128, 1, false>); allow(attn_few_kernel<128, 2, false>); allow(attn_few_kernel<128, 1, true>);
+  allow(attn_few_kernel<64, 1, false>); allow(attn_few_kernel<64, 2, false>); allow(attn_few_kernel<64, 1, true>);
+  return e;
+}
+
+cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, cudaStream_t st) {
+  const int nt = few_tiles_of(a.d, a.rcap, f32);
+  a.grid = ctx->num_sms * few_ctas(nt, f32);
+  a.min_blocks = 2 * FEW_WARPS;
+  attn_place(a, 8 * nt, ws);
+  if (a.d.Dh == 128) return f32 ? launch_few<128, 1, true>(ctx, a, st) : nt == 2 ? launch_few<128, 2, false>(ctx, a, st) : launch_few<128, 1, false>(ctx, a, st);
+  return f32 ? launch_few<64, 1, true>(ctx, a, st) : nt == 2 ? launch_few<64, 2, false>(ctx, a, st) : launch_few<64, 1, false>(ctx, a, st);
+}
+
+}  // namespace ts
+
+using namespace ts;
+
+extern "C" size_t ts_tree_attention_workspace_bytes(const ts_ctx* ctx, const ts_cache_layout* lay, int32_t B) {
+  if (!ctx || cache_layout_error(lay) || B < 1 || B > ctx->cfg.max_batch) return 0;
+  return attn_few_workspace(ctx, cache_dims(lay), lay->dtype == TS_DTYPE_F32);
+}
+
+extern "C" int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* lay, int32_t B, const void* q, int64_t ldq, const void* pool,
+                                     const int32_t* block_table, const int32_t* seq_len, const int32_t* n_nodes, const uint64_t* mask,
+                                     float scale, void* out, int64_t ldo, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  if (!ctx) return set_error(TS_ERR_INVALID, "ts_tree_attention: null context");
+  if (cache_layout_error(lay)) return set_layout_error("ts_tree_attention", lay);
+  const void* req[] = {q, pool, out, ws};
+  for (const void* p : req)
+    if (bad_ptr(p)) return set_error(TS_ERR_INVALID, "ts_tree_attention: null or misaligned pointer");
+  if (bad_ptr4(block_table) || bad_ptr4(seq_len) || (n_nodes && bad_ptr4(n_nodes)) || (lse && bad_ptr4(lse)) || ((uintptr_t)mask & 7u))
+    return set_error(TS_ERR_INVALID, "ts_tree_attention: null or misaligned pointer");
+  if (mask && !n_nodes) return set_error(TS_ERR_INVALID, "ts_tree_attention: a mask needs n_nodes");
+  if (B < 1 || B > ctx->cfg.max_batch) return set_error(TS_ERR_INVALID, "ts_tree_attention: B out of range");
+  const bool f32 = lay->dtype == TS_DTYPE_F32;
+  const int64_t unit = f32 ? 4 : 8, least = (int64_t)lay->Hq * lay->Dh;
+  if (ldq < least || ldo < least || ldq % unit || ldo % unit) return set_error(TS_ERR_INVALID, "ts_tree_attention: row strides must cover Hq * Dh elements and be multiples of 16 bytes");
+  if (!(fabsf(scale) <= 1e30f)) return set_error(TS_ERR_INVALID, "ts_tree_attention: scale must be finite");
+  if (ws_bytes < ts_tree_attention_workspace_bytes(ctx, lay, B)) return set_error(TS_ERR_WORKSPACE, "ts_tree_attention: workspace too small");
+  if (!on_ctx_device(ctx)) return set_error(TS_ERR_INVALID, "ts_tree_attention: the context's device is not the current one");
+  AttnArgs a{};
+  a.d = cache_dims(lay);
+  a.B = B; a.rcap = n_nodes ? ctx->cfg.Nmax + 1 : 1; a.N = ctx->cfg.Nmax; a.words = (ctx->cfg.Nmax + 63) / 64;
+  a.q = q; a.ldq = ldq; a.pool = (const unsigned char*)pool; a.table = block_table; a.seq_len = seq_len; a.n_nodes = n_nodes; a.mask = mask;
+  a.qk = ldexpf(scale * LOG2E, K_SHIFT + lay->k_exp); a.vo = ldexpf(1.f, V_SHIFT + lay->v_exp);
+  a.out = out; a.ldo = ldo; a.lse = lse; a.limit = ctx->wait_limit;
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e = attn_few_launch(ctx, a, f32, (char*)ws, st);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  return e == cudaSuccess ? TS_OK : set_cuda_error("ts_tree_attention", e);
+}
