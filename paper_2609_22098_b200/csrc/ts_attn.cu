@@ -12,14 +12,17 @@ namespace ts {
 // ------------------------------------------------------------------------------------------------
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
+constexpr int FEW_BLOCKS = 2;                        // blocks a warp takes in a step: two score chains side by side
+constexpr int FEW_TOKENS = FEW_BLOCKS * CACHE_BLOCK;
 
 template <int Dh, int NT>
 struct FewPlan {
   static constexpr int QT = 8 * NT;
   static constexpr int BLK = cache_block_bytes(Dh);
-  static constexpr int STAGES = 4;
+  static constexpr int STEP = FEW_BLOCKS * BLK;
+  static constexpr int STAGES = 3;
   static constexpr int ROW = Dh + 4;                       // floats between rows of the merge buffer
-  static constexpr int RING = FEW_WARPS * STAGES * BLK;
+  static constexpr int RING = FEW_WARPS * STAGES * STEP;
   static constexpr int MERGE = FEW_WARPS * QT * (ROW + 2) * 4;
   static constexpr int SMEM = RING + MERGE;
 };
@@ -91,17 +94,114 @@ struct Queries {
   }
 };
 
+// Scores of a block's 16 tokens, before the factors of the columns: rows g, g + 8 (tokens), columns 2t, 2t + 1 (queries).
+template <int Dh, int NT, bool F32>
+__device__ __forceinline__ void score_block(const unsigned char* blk, const Queries<Dh, NT, F32>& q, float (&s)[NT][4], int g, int t) {
+  constexpr int KW = Dh / 32;        // words of a token's K codes that a lane holds
+#pragma unroll
+  for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+  uint32_t kw[2][KW];
+  __half2 sc[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const unsigned char* row = blk + (g + 8 * e) * (Dh / 2) + t * (Dh / 8);
+    if (Dh == 128) {
+      const uint4 v = *reinterpret_cast<const uint4*>(row);
+      kw[e][0] = v.x; kw[e][1] = v.y; kw[e][KW - 2] = v.z; kw[e][KW - 1] = v.w;
+    } else {
+      const uint2 v = *reinterpret_cast<const uint2*>(row);
+      kw[e][0] = v.x; kw[e][1] = v.y;
+    }
+    const unsigned char* sp = blk + off_ks(Dh) + (g + 8 * e) * (Dh / CACHE_GROUP) + t * (Dh / 64);
+    sc[e] = k_scales(Dh == 128 ? *reinterpret_cast<const unsigned short*>(sp) : *sp);
+  }
+#pragma unroll
+  for (int i = 0; i < KW; ++i) {
+    uint32_t x[2][4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const __half2 ss = Dh == 128 && i >= KW / 2 ? __high2half2(sc[e]) : __low2half2(sc[e]);
+      unpack8(kw[e][i], ss, __hmul2(ss, __float2half2_rn(-1032.f)), __hmul2(ss, __float2half2_rn(-72.f)), x[e]);
+    }
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const uint32_t fr[4] = {x[0][2 * v], x[1][2 * v], x[0][2 * v + 1], x[1][2 * v + 1]};
+      const int r = 4 * i + 2 * v;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if (F32) {
+          // each step's sum apart and added in fp32: the instruction's own accumulation rounds towards zero
+          float c[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_16816(c, fr, q.lo[F32 ? n : 0][F32 ? r : 0], q.lo[F32 ? n : 0][F32 ? r + 1 : 0]);
+          mma_16816(c, fr, q.hi[n][r], q.hi[n][r + 1]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) s[n][k] += c[k];
+        } else {
+          mma_16816(s[n], fr, q.hi[n][r], q.hi[n][r + 1]);
+        }
+      }
+    }
+  }
+}
+
+// O^T += V^T P^T for a block: lane (g, t) holds Dh/8 channels of tokens 2t, 2t + 1 of both octets.
+template <int Dh, int NT, bool F32>
+__device__ __forceinline__ void value_block(const unsigned char* blk, const uint32_t (&ph)[NT][2], const uint32_t (&pl)[F32 ? NT : 1][2], float (&o)[NT][Dh / 16][4], int g, int t) {
+  constexpr int VW = Dh / 64;   // words of a token that a lane holds
+  uint32_t va[2][VW], vb[2][VW];
+  __half2 vs[2], c1032[2], c72[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const unsigned char* oct = blk + off_vc(Dh) + e * (4 * Dh);
+    if (Dh == 128) {
+      const uint4 v = *reinterpret_cast<const uint4*>(oct + g * 64 + t * 16);
+      va[e][0] = v.x; va[e][VW - 1] = v.y; vb[e][0] = v.z; vb[e][VW - 1] = v.w;
+    } else {
+      va[e][0] = *reinterpret_cast<const uint32_t*>(oct + (g >> 1) * 64 + t * 16 + (g & 1) * 4);
+      vb[e][0] = *reinterpret_cast<const uint32_t*>(oct + (g >> 1) * 64 + t * 16 + 8 + (g & 1) * 4);
+    }
+    vs[e] = v_scales(*reinterpret_cast<const unsigned short*>(blk + off_vs(Dh) + e * (Dh / 2) + (Dh == 128 ? g : g >> 1) * 8 + 2 * t));
+    c1032[e] = __hmul2(vs[e], __float2half2_rn(-1032.f));
+    c72[e] = __hmul2(vs[e], __float2half2_rn(-72.f));
+  }
+#pragma unroll
+  for (int i = 0; i < VW; ++i) {
+    uint32_t lo[2][4], hi[2][4];   // even and odd channels of the word, tokens in the halves
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      unpack8(__byte_perm(va[e][i], vb[e][i], 0x5410), vs[e], c1032[e], c72[e], lo[e]);
+      unpack8(__byte_perm(va[e][i], vb[e][i], 0x7632), vs[e], c1032[e], c72[e], hi[e]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t fr[4] = {lo[0][j], hi[0][j], lo[1][j], hi[1][j]};
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float* acc = o[n][4 * i + j];
+        if (F32) {
+          float c[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_16816(c, fr, pl[F32 ? n : 0][0], pl[F32 ? n : 0][1]);
+          mma_16816(c, fr, ph[n][0], ph[n][1]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[k] += c[k];
+        } else {
+          mma_16816(acc, fr, ph[n][0], ph[n][1]);
+        }
+      }
+    }
+  }
+}
+
 template <int Dh, int NT, bool F32>
 __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_kernel(const AttnArgs a) {
   using P = FewPlan<Dh, NT>;
   using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
   constexpr int QT = P::QT, ST = P::STAGES, BLK = P::BLK;
   constexpr int MT = Dh / 16;        // tiles of 16 channels
-  constexpr int KW = Dh / 32;        // words of a token's K codes that a lane holds
   constexpr float ROOM = F32 ? 0.f : 8.f, LIFT = F32 ? 15.f : 7.f;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ uint64_t bars[FEW_WARPS][ST];
-  __shared__ int present[FEW_WARPS][ST];
+  __shared__ int present[FEW_WARPS][ST];   // a bit for each block of the step
   __shared__ int gave_up;
   float* merge = reinterpret_cast<float*>(smem + P::RING);
   float* merge_ml = merge + FEW_WARPS * QT * P::ROW;
@@ -117,35 +217,46 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
   AttnUnit u;
   long long start, end;
   int active;
-  if (!attn_locate<FEW_THREADS>(a, QT, u, start, end, active)) return;
+  if (!attn_locate<QT, FEW_TOKENS, FEW_THREADS>(a, u, start, end, active)) return;
 
-  // The copies run ahead of the arithmetic, across units: cursor and page of the block to fetch next.
-  unsigned char* ring = smem + w * ST * BLK;
+  // The copies run ahead of the arithmetic, across units: the warp's steps are w, w + 4, .. of the CTA's piece.  The cursor
+  // stands at step fj of unit fu, in column fc and block fin of that page; the table's entries are read a step ahead.
+  unsigned char* ring = smem + w * ST * P::STEP;
+  const int per = a.d.ps / CACHE_BLOCK, adv = FEW_WARPS * FEW_BLOCKS, adv_c = adv / per, adv_in = adv - adv_c * per;
   AttnUnit fu = u;
-  long long fp = start + w;
-  int fpage = -1, finner = 0, fslot = 0;
-  const int per = a.d.ps / CACHE_BLOCK;
+  int fj = (int)(start - u.t0) + w, fleft = (int)(end - start) - w, fc = fj * FEW_BLOCKS / per, fin = fj * FEW_BLOCKS - fc * per, fh = fu.v / fu.nq;
+  int fslot = 0, copies = 0, page0 = -1, page1 = -1;
   auto look_up = [&]() {
-    if (fp >= end) return;
-    while (fp >= fu.t0 + fu.nblk) next_unit(a, QT, fu);
-    const int j = (int)(fp - fu.t0), c = j / per;
-    finner = j - c * per;
-    fpage = c < a.d.cols ? __ldg(a.table + (size_t)fu.b * a.d.cols + c) : -1;
+    if (fleft <= 0) return;
+    if (fj >= fu.n) {
+      do {
+        fj -= fu.n;
+        next_unit<QT, FEW_TOKENS>(a, fu);
+      } while (fj >= fu.n);
+      fc = fj * FEW_BLOCKS / per; fin = fj * FEW_BLOCKS - fc * per; fh = fu.v / fu.nq;
+    }
+    const int* row = a.table + (size_t)fu.b * a.d.cols;
+    const int c1 = fin + 1 < per ? fc : fc + 1;
+    const unsigned last = (unsigned)fu.seq + (unsigned)fu.rows - 1u;   // the request's last token; a block behind it is not fetched
+    page0 = fc < a.d.cols ? __ldg(row + fc) : -1;
+    page1 = c1 < a.d.cols && (unsigned)(fj * FEW_BLOCKS + 1) * CACHE_BLOCK <= last ? __ldg(row + c1) : -1;
   };
   auto fetch = [&]() {
-    if (fp < end) {
-      if (lane == 0) {
-        const long long off = block_offset(a.d, fpage, finner, fu.v / fu.nq);
-        present[w][fslot] = off >= 0;
-        if (off >= 0) {
-          mbar_expect_tx(&bars[w][fslot], BLK);
-          bulk_load(ring + fslot * BLK, a.pool + off, BLK, &bars[w][fslot]);
-        } else mbar_arrive(&bars[w][fslot]);
-      }
-      fp += FEW_WARPS;
-      if (++fslot == ST) fslot = 0;
-      look_up();
+    if (fleft <= 0) return;
+    if (lane == 0) {
+      const long long off0 = block_offset(a.d, page0, fin, fh), off1 = block_offset(a.d, page1, fin + 1 < per ? fin + 1 : 0, fh);
+      present[w][fslot] = (off0 >= 0 ? 1 : 0) | (off1 >= 0 ? 2 : 0);
+      uint64_t* bar = &bars[w][fslot];
+      mbar_expect_tx(bar, (off0 >= 0 ? BLK : 0) + (off1 >= 0 ? BLK : 0));
+      if (off0 >= 0) bulk_load(ring + fslot * P::STEP, a.pool + off0, BLK, bar);
+      if (off1 >= 0) bulk_load(ring + fslot * P::STEP + BLK, a.pool + off1, BLK, bar);
     }
+    ++copies;
+    if (++fslot == ST) fslot = 0;
+    fj += FEW_WARPS; fleft -= FEW_WARPS;
+    fc += adv_c; fin += adv_in;
+    if (fin >= per) { fin -= per; ++fc; }
+    look_up();
   };
   look_up();
 #pragma unroll
@@ -153,10 +264,13 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 
   int slot = 0;
   uint32_t phase = 0;
-  long long pos = start, p = start + w;
-  while (pos < end) {
+  int mine = w;                                   // the warp's next step, counted from the CTA's first
+  const int steps = (int)(end - start);
+  int pos = 0;                                    // the segment's first
+  while (pos < steps) {
     const int h = u.v / u.nq, first = (u.v - h * u.nq) * QT;
-    const long long t1 = u.t0 + u.nblk, seg_end = min(t1, end);
+    const int j0 = (int)(start + pos - u.t0);     // step of the unit at which the segment begins
+    const int seg = min(u.n - j0, steps - pos);
     Queries<Dh, NT, F32> q;
     q.load(a, u, h, first, lane);
     float o[NT][MT][4], m[NT][2], ref[NT][2], l[NT][2];
@@ -168,151 +282,74 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
         for (int c = 0; c < 4; ++c) o[n][i][c] = 0.f;
       m[n][0] = m[n][1] = -INFINITY; ref[n][0] = ref[n][1] = 0.f; l[n][0] = l[n][1] = 0.f;
     }
-    for (; p < seg_end; p += FEW_WARPS) {
+    for (; mine < pos + seg; mine += FEW_WARPS) {
       const bool ok = mbar_wait(&bars[w][slot], phase, (volatile int*)&gave_up, nullptr, a.limit);
-      const bool here = present[w][slot] != 0;
-      const unsigned char* blk = ring + slot * BLK;
-      // ---- scores of 16 tokens: s[n] = rows g, g + 8 (tokens), columns 2t, 2t + 1 (queries)
-      float s[NT][4];
+      const int here = present[w][slot];
+      const unsigned char* blk = ring + slot * P::STEP;
+      float s[FEW_BLOCKS][NT][4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-      {
-        uint32_t kw[2][KW];
-        __half2 sc[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const unsigned char* row = blk + (g + 8 * e) * (Dh / 2) + t * (Dh / 8);
-          if (Dh == 128) {
-            const uint4 v = *reinterpret_cast<const uint4*>(row);
-            kw[e][0] = v.x; kw[e][1] = v.y; kw[e][KW - 2] = v.z; kw[e][KW - 1] = v.w;
-          } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(row);
-            kw[e][0] = v.x; kw[e][1] = v.y;
-          }
-          const unsigned char* sp = blk + off_ks(Dh) + (g + 8 * e) * (Dh / CACHE_GROUP) + t * (Dh / 64);
-          sc[e] = k_scales(Dh == 128 ? *reinterpret_cast<const unsigned short*>(sp) : *sp);
-        }
-#pragma unroll
-        for (int i = 0; i < KW; ++i) {
-          uint32_t x[2][4];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const __half2 ss = Dh == 128 && i >= KW / 2 ? __high2half2(sc[e]) : __low2half2(sc[e]);
-            unpack8(kw[e][i], ss, __hmul2(ss, __float2half2_rn(-1032.f)), __hmul2(ss, __float2half2_rn(-72.f)), x[e]);
-          }
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const uint32_t fr[4] = {x[0][2 * v], x[1][2 * v], x[0][2 * v + 1], x[1][2 * v + 1]};
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const int r = 4 * i + 2 * v;
-              if (F32) {
-                // each step's sum apart and added in fp32: the instruction's own accumulation rounds towards zero
-                float c[4] = {0.f, 0.f, 0.f, 0.f};
-                mma_16816(c, fr, q.lo[F32 ? n : 0][F32 ? r : 0], q.lo[F32 ? n : 0][F32 ? r + 1 : 0]);
-                mma_16816(c, fr, q.hi[n][r], q.hi[n][r + 1]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) s[n][k] += c[k];
-              } else {
-                mma_16816(s[n], fr, q.hi[n][r], q.hi[n][r + 1]);
-              }
-            }
-          }
-        }
-      }
+      for (int k = 0; k < FEW_BLOCKS; ++k) score_block<Dh, NT, F32>(blk + k * BLK, q, s[k], g, t);
       // ---- weights
-      const int tok0 = (int)(p - u.t0) * CACHE_BLOCK;
-      const bool masked = tok0 > u.seq - CACHE_BLOCK || !here || !ok;
-      uint32_t ph[NT][2], pl[F32 ? NT : 1][2];
+      const int tok0 = (j0 + mine - pos) * FEW_TOKENS;
+      const bool masked = tok0 > u.seq - FEW_TOKENS || here != (1 << FEW_BLOCKS) - 1 || !ok;
+      uint32_t ph[FEW_BLOCKS][NT][2], pl[FEW_BLOCKS][F32 ? NT : 1][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[n][c] *= q.f[n][c & 1];
+        for (int k = 0; k < FEW_BLOCKS; ++k)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[k][n][c] *= q.f[n][c & 1];
         if (masked) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const int rel = tok0 + g + 8 * (c >> 1) - u.seq, idx = first + 8 * n + 2 * t + (c & 1);
-            const bool sees = here && (rel < 0 || row_sees(a, u.b, idx / a.d.G, rel, u.rows));
-            if (!sees) s[n][c] = -INFINITY;
-            if (!ok) s[n][c] = NAN;
-          }
+          for (int k = 0; k < FEW_BLOCKS; ++k)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const int rel = tok0 + k * CACHE_BLOCK + g + 8 * (c >> 1) - u.seq, idx = first + 8 * n + 2 * t + (c & 1);
+              const bool sees = ((here >> k) & 1) && (rel < 0 || row_sees(a, u.b, idx / a.d.G, rel, u.rows));
+              if (!sees) s[k][n][c] = -INFINITY;
+              if (!ok) s[k][n][c] = NAN;
+            }
         }
         // The reference of the exponents moves only when a score passes it by more than ROOM: weights stay below
         // 2^(ROOM + LIFT) = 2^15, and LIFT keeps small ones out of fp16's subnormals.
-        const bool up = fmaxf(s[n][0], s[n][2]) > m[n][0] || fmaxf(s[n][1], s[n][3]) > m[n][1];
-        if (__any_sync(~0u, up)) {
+        float top[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          top[c] = fmaxf(s[0][n][c], s[0][n][c + 2]);
+#pragma unroll
+          for (int k = 1; k < FEW_BLOCKS; ++k) top[c] = fmaxf(top[c], fmaxf(s[k][n][c], s[k][n][c + 2]));
+        }
+        if (__any_sync(~0u, top[0] > m[n][0] || top[1] > m[n][1])) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float top = fmaxf(s[n][c], s[n][c + 2]);
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
-            if (top > m[n][c]) {
-              const float r = m[n][c] == -INFINITY ? 0.f : ex2(ref[n][c] - (top - LIFT));
-              m[n][c] = top + ROOM; ref[n][c] = top - LIFT;
+            for (int x = 4; x < 32; x <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(~0u, top[c], x));
+            if (top[c] > m[n][c]) {
+              const float r = m[n][c] == -INFINITY ? 0.f : ex2(ref[n][c] - (top[c] - LIFT));
+              m[n][c] = top[c] + ROOM; ref[n][c] = top[c] - LIFT;
               l[n][c] *= r;
 #pragma unroll
               for (int i = 0; i < MT; ++i) { o[n][i][c] *= r; o[n][i][c + 2] *= r; }
             }
           }
         }
-        float e[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) e[c] = ex2(s[n][c] - ref[n][c & 1]);
-        l[n][0] += e[0] + e[2]; l[n][1] += e[1] + e[3];
-        const __half2 h0 = __floats2half2_rn(e[0], e[1]), h1 = __floats2half2_rn(e[2], e[3]);
-        ph[n][0] = transpose8(as_u32(h0)); ph[n][1] = transpose8(as_u32(h1));
-        if (F32) {
-          pl[F32 ? n : 0][0] = transpose8(as_u32(__floats2half2_rn(e[0] - __low2float(h0), e[1] - __high2float(h0))));
-          pl[F32 ? n : 0][1] = transpose8(as_u32(__floats2half2_rn(e[2] - __low2float(h1), e[3] - __high2float(h1))));
-        }
-      }
-      // ---- O^T += V^T P^T: lane (g, t) holds Dh/8 channels of tokens 2t, 2t + 1 of both octets
-      {
-        constexpr int VW = Dh / 64;   // words of a token that a lane holds
-        uint32_t va[2][VW], vb[2][VW];
-        __half2 vs[2], c1032[2], c72[2];
+        for (int k = 0; k < FEW_BLOCKS; ++k) {
+          float e[4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const unsigned char* oct = blk + off_vc(Dh) + e * (4 * Dh);
-          if (Dh == 128) {
-            const uint4 v = *reinterpret_cast<const uint4*>(oct + g * 64 + t * 16);
-            va[e][0] = v.x; va[e][VW - 1] = v.y; vb[e][0] = v.z; vb[e][VW - 1] = v.w;
-          } else {
-            va[e][0] = *reinterpret_cast<const uint32_t*>(oct + (g >> 1) * 64 + t * 16 + (g & 1) * 4);
-            vb[e][0] = *reinterpret_cast<const uint32_t*>(oct + (g >> 1) * 64 + t * 16 + 8 + (g & 1) * 4);
-          }
-          vs[e] = v_scales(*reinterpret_cast<const unsigned short*>(blk + off_vs(Dh) + e * (Dh / 2) + (Dh == 128 ? g : g >> 1) * 8 + 2 * t));
-          c1032[e] = __hmul2(vs[e], __float2half2_rn(-1032.f));
-          c72[e] = __hmul2(vs[e], __float2half2_rn(-72.f));
-        }
-#pragma unroll
-        for (int i = 0; i < VW; ++i) {
-          uint32_t lo[2][4], hi[2][4];   // even and odd channels of the word, tokens in the halves
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            unpack8(__byte_perm(va[e][i], vb[e][i], 0x5410), vs[e], c1032[e], c72[e], lo[e]);
-            unpack8(__byte_perm(va[e][i], vb[e][i], 0x7632), vs[e], c1032[e], c72[e], hi[e]);
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t fr[4] = {lo[0][j], hi[0][j], lo[1][j], hi[1][j]};
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              float* acc = o[n][4 * i + j];
-              if (F32) {
-                float c[4] = {0.f, 0.f, 0.f, 0.f};
-                mma_16816(c, fr, pl[F32 ? n : 0][0], pl[F32 ? n : 0][1]);
-                mma_16816(c, fr, ph[n][0], ph[n][1]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) acc[k] += c[k];
-              } else {
-                mma_16816(acc, fr, ph[n][0], ph[n][1]);
-              }
-            }
+          for (int c = 0; c < 4; ++c) e[c] = ex2(s[k][n][c] - ref[n][c & 1]);
+          l[n][0] += e[0] + e[2]; l[n][1] += e[1] + e[3];
+          const __half2 h0 = __floats2half2_rn(e[0], e[1]), h1 = __floats2half2_rn(e[2], e[3]);
+          ph[k][n][0] = transpose8(as_u32(h0)); ph[k][n][1] = transpose8(as_u32(h1));
+          if (F32) {
+            pl[k][F32 ? n : 0][0] = transpose8(as_u32(__floats2half2_rn(e[0] - __low2float(h0), e[1] - __high2float(h0))));
+            pl[k][F32 ? n : 0][1] = transpose8(as_u32(__floats2half2_rn(e[2] - __low2float(h1), e[3] - __high2float(h1))));
           }
         }
       }
-      __syncwarp();   // every lane has read the slot that the next copy goes to
+#pragma unroll
+      for (int k = 0; k < FEW_BLOCKS; ++k) value_block<Dh, NT, F32>(blk + k * BLK, ph[k], pl[k], o, g, t);
+      __syncwarp();   // every lane has read the slot that the next copies go to
       if (++slot == ST) { slot = 0; phase ^= 1u; }
       fetch();
     }
@@ -330,7 +367,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
         for (int i = 0; i < MT; ++i) *reinterpret_cast<float2*>(merge + row * P::ROW + g * (Dh / 8) + 2 * i) = make_float2(o[n][i][c], o[n][i][c + 2]);
       }
     __syncthreads();
-    const bool whole = pos == u.t0 && seg_end == t1;
+    const bool whole = seg == u.n;
     const size_t piece = ((size_t)blockIdx.x * 2 + (start > u.t0 ? 0 : 1)) * QT;
     for (int e = threadIdx.x; e < QT * Dh; e += FEW_THREADS) {
       const int row = e / Dh, ch = e - row * Dh, idx = first + row;
@@ -353,13 +390,13 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
       }
     }
     __syncthreads();
-    pos = seg_end;
-    if (pos < end) next_unit(a, QT, u);
+    pos += seg;
+    if (pos < steps) next_unit<QT, FEW_TOKENS>(a, u);
   }
   // after a wait that gave up copies may still be on their way into this CTA's memory
   if (gave_up)
     for (int s = 0; s < ST; ++s) {
-      const int n = (int)(((fp - start - w) / FEW_WARPS + ST - 1 - s) / ST);   // copies that went to the slot
+      const int n = (copies + ST - 1 - s) / ST;   // steps that went to the slot
       for (uint32_t i = 0; n > 0 && i < a.limit && !mbar_try_wait(&bars[w][s], (n - 1) & 1); ++i) __nanosleep(100);
     }
 }
@@ -465,7 +502,7 @@ cudaError_t attn_setup(ts_ctx* ctx) {
 cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, cudaStream_t st) {
   const int nt = few_tiles_of(a.d, a.rcap, f32);
   a.grid = ctx->num_sms * few_ctas(nt, f32);
-  a.min_blocks = 2 * FEW_WARPS;
+  a.min_steps = FEW_WARPS;
   attn_place(a, 8 * nt, ws);
   if (a.d.Dh == 128) return f32 ? launch_few<128, 1, true>(ctx, a, st) : nt == 2 ? launch_few<128, 2, false>(ctx, a, st) : launch_few<128, 1, false>(ctx, a, st);
   return f32 ? launch_few<64, 1, true>(ctx, a, st) : nt == 2 ? launch_few<64, 2, false>(ctx, a, st) : launch_few<64, 1, false>(ctx, a, st);

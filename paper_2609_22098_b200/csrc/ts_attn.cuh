@@ -1,7 +1,7 @@
 // What the attention kernels over the 4-bit cache share: how the work is cut, who sees what, how pieces are joined.
 //
-// The work is a line of blocks (16 tokens of one head for one tile of query rows): requests, then kv heads, then tiles of
-// rows, then blocks.  A unit = the blocks of one (request, head, tile).  The line is cut into equal pieces, one a CTA,
+// The work is a line of steps (a few blocks of one head for one tile of query rows): requests, then kv heads, then tiles of
+// rows, then steps.  A unit = the steps of one (request, head, tile).  The line is cut into equal pieces, one a CTA,
 // whatever the lengths are: lengths are known on the device only.  A unit that lies within one CTA is written by it; the
 // pieces of another go to the workspace, with a record by which the join kernel finds them.
 #pragma once
@@ -24,48 +24,51 @@ struct AttnArgs {
   float* lse;
   struct AttnRecord* records; float* part; float* part_ml;   // workspace: [grid], [grid][2][QT][Dh], [grid][2][QT][2]
   int grid;                // CTAs at most
-  int min_blocks;          // blocks that make a piece worth a CTA of its own
+  int min_steps;           // steps that make a piece worth a CTA of its own
   unsigned limit;          // polls before a wait gives up
 };
 
 // pieces first..last of a unit; first < 0: nothing begins here that is to be joined
 struct AttnRecord { int b, v, first, last; long long t0; int nq, active; };
 
-struct AttnUnit { int b, v, nblk, nq, rows, seq; long long t0; };   // v = head * nq + tile; t0 = place of its first block
+struct AttnUnit { int b, v, n, nq, rows, seq; long long t0; };   // v = head * nq + tile; n steps, the first at place t0
 
-__device__ __forceinline__ long long unit_blocks(const AttnArgs& a, int b, int QT, AttnUnit& u) {
+// QT query rows a tile, TOK tokens a step
+template <int QT, int TOK>
+__device__ __forceinline__ long long unit_steps(const AttnArgs& a, int b, AttnUnit& u) {
   u.b = b; u.seq = a.seq_len[b];
   u.rows = request_rows(a.n_nodes, b, a.rcap);
-  if (u.seq < 0) { u.nblk = 0; u.nq = 0; return 0; }
+  if (u.seq < 0) { u.n = 0; u.nq = 0; return 0; }
   const long long end = min((long long)u.seq + u.rows, (long long)a.d.cols * a.d.ps);   // (no page beyond the table's)
-  u.nblk = (int)max(1ll, (end + CACHE_BLOCK - 1) / CACHE_BLOCK);
+  u.n = (int)max(1ll, (end + TOK - 1) / TOK);
   u.nq = (u.rows * a.d.G + QT - 1) / QT;
-  return (long long)a.d.Hkv * u.nq * u.nblk;
+  return (long long)a.d.Hkv * u.nq * u.n;
 }
 
 // CTAs that take part, and where piece c begins
-__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, total / a.min_blocks)); }
+__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, total / a.min_steps)); }
 __device__ __forceinline__ long long piece_start(long long total, int active, int c) { return total * c / active; }
 
-__device__ __forceinline__ void next_unit(const AttnArgs& a, int QT, AttnUnit& u) {
-  u.t0 += u.nblk;
+template <int QT, int TOK>
+__device__ __forceinline__ void next_unit(const AttnArgs& a, AttnUnit& u) {
+  u.t0 += u.n;
   if (++u.v < a.d.Hkv * u.nq) return;
   u.v = 0;
   while (++u.b < a.B) {
     AttnUnit n = u;
-    if (unit_blocks(a, u.b, QT, n) > 0) { n.t0 = u.t0; n.v = 0; u = n; return; }
+    if (unit_steps<QT, TOK>(a, u.b, n) > 0) { n.t0 = u.t0; n.v = 0; u = n; return; }
   }
 }
 
 // Finds the whole line's length and the unit in which this CTA's piece begins.  All threads call it; false: no piece.
-template <int THREADS>
-__device__ bool attn_locate(const AttnArgs& a, int QT, AttnUnit& u, long long& start, long long& end, int& active) {
+template <int QT, int TOK, int THREADS>
+__device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, long long& end, int& active) {
   __shared__ long long wsum[THREADS / 32];
   __shared__ AttnUnit found;
   const int per = (a.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   AttnUnit n;
   long long sum = 0;
-  for (int b = b0; b < min(b0 + per, a.B); ++b) sum += unit_blocks(a, b, QT, n);
+  for (int b = b0; b < min(b0 + per, a.B); ++b) sum += unit_steps<QT, TOK>(a, b, n);
   long long inc = sum;
   for (int o = 1; o < 32; o <<= 1) {
     const long long v = __shfl_up_sync(~0u, inc, o);
@@ -88,10 +91,10 @@ __device__ bool attn_locate(const AttnArgs& a, int QT, AttnUnit& u, long long& s
   long long at = before + inc - sum;
   if (start >= at && start < at + sum)
     for (int b = b0;; ++b) {
-      const long long w = unit_blocks(a, b, QT, n);
+      const long long w = unit_steps<QT, TOK>(a, b, n);
       if (start < at + w) {
-        n.v = (int)((start - at) / n.nblk);
-        n.t0 = at + (long long)n.v * n.nblk;
+        n.v = (int)((start - at) / n.n);
+        n.t0 = at + (long long)n.v * n.n;
         found = n;
         break;
       }
@@ -104,7 +107,7 @@ __device__ bool attn_locate(const AttnArgs& a, int QT, AttnUnit& u, long long& s
     AttnRecord r{u.b, u.v, -1, 0, u.t0, u.nq, active};
     if (start > u.t0 && piece_start(total, active, blockIdx.x - 1) <= u.t0) {
       r.first = blockIdx.x - 1;
-      r.last = (int)(((u.t0 + u.nblk) * active + total - 1) / total) - 1;   // the last c with start(c) < end of the unit
+      r.last = (int)(((u.t0 + u.n) * active + total - 1) / total) - 1;   // the last c with start(c) < end of the unit
     }
     a.records[blockIdx.x] = r;
   }

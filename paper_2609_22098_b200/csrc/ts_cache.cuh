@@ -44,10 +44,11 @@ __device__ __forceinline__ int request_rows(const int* n_nodes, int b, int rcap)
   return n_nodes ? min(max(n_nodes[b], 0), rcap - 1) + 1 : 1;
 }
 
-// Byte address of block `blk` (of the request's tokens) of head h, -1 where the table has no page for it.
+// Byte address of block `inner` of a page for head h, -1 where the table's entry is no page.
 __device__ __forceinline__ long long block_offset(const CacheDims& d, int page, int inner, int h) {
   if ((unsigned)page >= (unsigned)d.n_pages) return -1;
-  return (long long)page * (long long)d.page_bytes() + (long long)(h * (d.ps / CACHE_BLOCK) + inner) * cache_block_bytes(d.Dh);
+  const unsigned per = d.ps / CACHE_BLOCK;   // (a page has less than 2^32 bytes: 1,024 heads, 4,096 tokens, 144 bytes each)
+  return ((long long)((unsigned long long)(unsigned)page * ((unsigned)d.Hkv * per)) + (unsigned)h * per + (unsigned)inner) * cache_block_bytes(d.Dh);
 }
 
 // Eight codes of a word as four half2 of (c - 8) * s, times the power of two that s carries: h[j] = elements 2j, 2j + 1.
