@@ -402,64 +402,85 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 }
 
 // ------------------------------------------------------------------------------------------------
-// Join: one CTA a (cut unit, query row).  The pieces are added in their order, so results do not depend on timing.
+// Join: RW warps a (cut unit, query row).  The pieces are added in their order, so results do not depend on timing.
 // ------------------------------------------------------------------------------------------------
-constexpr int JOIN_WARPS = 4;
+constexpr int JOIN_WARPS = 8;
 
-template <int Dh, typename T>
+template <int Dh, int RW, typename T>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnArgs a, int QT) {
-  constexpr int V = Dh / 32;
+  constexpr int V = Dh / 32, ROWS = JOIN_WARPS / RW;
   __shared__ float acc[JOIN_WARPS][Dh], red[JOIN_WARPS][2];
   pdl_wait();
   pdl_launch_dependents();
   const AttnRecord r = a.records[blockIdx.x];
   if (r.first < 0) return;
-  const int h = r.v / r.nq, row = blockIdx.y, idx = (r.v - h * r.nq) * QT + row;
-  if (idx >= request_rows(a.n_nodes, r.b, a.rcap) * a.d.G) return;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = r.last - r.first + 1;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, part = w % RW, w0 = w - part;
+  const int h = r.v / r.nq, row = blockIdx.y * ROWS + w / RW, idx = (r.v - h * r.nq) * QT + row, n = r.last - r.first + 1;
+  const bool used = idx < request_rows(a.n_nodes, r.b, a.rcap) * a.d.G;
   // piece k: the first begins at or before the unit and is its CTA's last; the others begin within it
   auto at = [&](int k) { return ((size_t)(r.first + k) * 2 + (k == 0 ? 1 : 0)) * QT + row; };
   float top = -INFINITY;
-  for (int k = threadIdx.x; k < n; k += JOIN_WARPS * 32) top = fmaxf(top, a.part_ml[2 * at(k)]);
+  if (used)
+    for (int k = part * 32 + lane; k < n; k += RW * 32) top = fmaxf(top, a.part_ml[2 * at(k)]);
 #pragma unroll
   for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
-  if (lane == 0) red[w][0] = top;
-  __syncthreads();
+  if (RW > 1) {
+    if (lane == 0) red[w][0] = top;
+    __syncthreads();
 #pragma unroll
-  for (int k = 0; k < JOIN_WARPS; ++k) top = fmaxf(top, red[k][0]);
+    for (int k = 0; k < RW; ++k) top = fmaxf(top, red[w0 + k][0]);
+  }
   float sum = 0.f, x[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = 0.f;
+  if (used) {
 #pragma unroll 4
-  for (int k = w; k < n; k += JOIN_WARPS) {
-    const float wgt = part_weight(a.part_ml[2 * at(k)], top);
-    sum += wgt * a.part_ml[2 * at(k) + 1];
+    for (int k = part; k < n; k += RW) {
+      const float wgt = part_weight(a.part_ml[2 * at(k)], top);
+      sum += wgt * a.part_ml[2 * at(k) + 1];
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] += wgt * a.part[at(k) * Dh + lane + 32 * i];
+      for (int i = 0; i < V; ++i) x[i] += wgt * a.part[at(k) * Dh + lane + 32 * i];
+    }
   }
+  if (RW > 1) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[w][lane + 32 * i] = x[i];
-  if (lane == 0) red[w][1] = sum;
-  __syncthreads();
-  sum = 0.f;
+    for (int i = 0; i < V; ++i) acc[w][lane + 32 * i] = x[i];
+    if (lane == 0) red[w][1] = sum;
+    __syncthreads();
+    if (part > 0 || !used) return;
 #pragma unroll
-  for (int k = 0; k < JOIN_WARPS; ++k) sum += red[k][1];
-  for (int ch = threadIdx.x; ch < Dh; ch += JOIN_WARPS * 32) {
-    float v = 0.f;
+    for (int k = 1; k < RW; ++k) {
+      sum += red[w0 + k][1];
 #pragma unroll
-    for (int k = 0; k < JOIN_WARPS; ++k) v += acc[k][ch];
-    store_out(reinterpret_cast<T*>(a.out) + out_row(a, r.b, h, idx) + ch, v * row_inv(sum) * a.vo);
+      for (int i = 0; i < V; ++i) x[i] += acc[w0 + k][lane + 32 * i];
+    }
   }
-  if (threadIdx.x == 0 && a.lse) a.lse[lse_row(a, r.b, h, idx)] = row_lse(top, sum);
+  if (!used) return;
+  T* out = reinterpret_cast<T*>(a.out) + out_row(a, r.b, h, idx);
+  const float inv = row_inv(sum) * a.vo;
+#pragma unroll
+  for (int i = 0; i < V; ++i) store_out(out + lane + 32 * i, x[i] * inv);
+  if (lane == 0 && a.lse) a.lse[lse_row(a, r.b, h, idx)] = row_lse(top, sum);
+}
+
+// Few rows are cut into more pieces: four warps a row there, two where tiles are large.
+cudaError_t attn_join(ts_ctx* ctx, const AttnArgs& a, int QT, bool f32, cudaStream_t st) {
+  ProfScope ps(ctx, K_ATTN_JOIN, st);
+  const int rw = QT > 16 ? 2 : 4;
+  void (*kernel)(const AttnArgs, int);
+  if (rw == 2) kernel = a.d.Dh == 128 ? attn_join_kernel<128, 2, __nv_bfloat16> : attn_join_kernel<64, 2, __nv_bfloat16>;
+  else if (f32) kernel = a.d.Dh == 128 ? attn_join_kernel<128, 4, float> : attn_join_kernel<64, 4, float>;
+  else kernel = a.d.Dh == 128 ? attn_join_kernel<128, 4, __nv_bfloat16> : attn_join_kernel<64, 4, __nv_bfloat16>;
+  return launch_kernel(kernel, dim3(a.grid, QT * rw / JOIN_WARPS), dim3(JOIN_WARPS * 32), 0, st, true, a, QT);
 }
 
 static size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-static size_t attn_workspace(int grid, int QT, int Dh) {
+size_t attn_workspace(int grid, int QT, int Dh) {
   return round256((size_t)grid * sizeof(AttnRecord)) + round256((size_t)grid * 2 * QT * Dh * 4) + round256((size_t)grid * 2 * QT * 2 * 4);
 }
 
-static void attn_place(AttnArgs& a, int QT, char* ws) {
+void attn_place(AttnArgs& a, int QT, char* ws) {
   a.records = (AttnRecord*)ws;
   a.part = (float*)(ws + round256((size_t)a.grid * sizeof(AttnRecord)));
   a.part_ml = (float*)((char*)a.part + round256((size_t)a.grid * 2 * QT * a.d.Dh * 4));
@@ -469,7 +490,7 @@ static void attn_place(AttnArgs& a, int QT, char* ws) {
 static int few_tiles_of(const CacheDims& d, int rcap, bool f32) { return !f32 && (long long)rcap * d.G > 8 ? 2 : 1; }
 static int few_ctas(int nt, bool f32) { return f32 || nt > 1 ? 2 : 3; }
 
-size_t attn_few_workspace(const ts_ctx* ctx, const CacheDims& d, bool f32) {
+static size_t attn_few_workspace(const ts_ctx* ctx, const CacheDims& d, bool f32) {
   size_t most = 0;
   for (int nt = 1; nt <= 2; ++nt) {
     const size_t n = attn_workspace(ctx->num_sms * few_ctas(nt, f32), 8 * nt, d.Dh);
@@ -486,9 +507,7 @@ static cudaError_t launch_few(ts_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
     ProfScope ps(ctx, K_ATTN_FEW, st);
     e = launch_kernel(attn_few_kernel<Dh, NT, F32>, dim3(a.grid), dim3(FEW_THREADS), P::SMEM, st, true, a);
   }
-  if (e != cudaSuccess) return e;
-  ProfScope ps(ctx, K_ATTN_JOIN, st);
-  return launch_kernel(attn_join_kernel<Dh, typename std::conditional<F32, float, __nv_bfloat16>::type>, dim3(a.grid, P::QT), dim3(JOIN_WARPS * 32), 0, st, true, a, P::QT);
+  return e != cudaSuccess ? e : attn_join(ctx, a, P::QT, F32, st);
 }
 
 cudaError_t attn_setup(ts_ctx* ctx) {
@@ -496,10 +515,11 @@ cudaError_t attn_setup(ts_ctx* ctx) {
   auto allow = [&](auto kernel) { if (e == cudaSuccess) e = allow_all_smem(kernel, ctx->max_smem); };
   allow(attn_few_kernel<128, 1, false>); allow(attn_few_kernel<128, 2, false>); allow(attn_few_kernel<128, 1, true>);
   allow(attn_few_kernel<64, 1, false>); allow(attn_few_kernel<64, 2, false>); allow(attn_few_kernel<64, 1, true>);
+  if (e == cudaSuccess) e = attn_many_setup(ctx);
   return e;
 }
 
-cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, cudaStream_t st) {
+static cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, cudaStream_t st) {
   const int nt = few_tiles_of(a.d, a.rcap, f32);
   a.grid = ctx->num_sms * few_ctas(nt, f32);
   a.min_steps = FEW_WARPS;
@@ -508,13 +528,18 @@ cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, cudaStr
   return f32 ? launch_few<64, 1, true>(ctx, a, st) : nt == 2 ? launch_few<64, 2, false>(ctx, a, st) : launch_few<64, 1, false>(ctx, a, st);
 }
 
+// Which kernel: tiles of 16 rows read the keys and values again for every tile, tiles of 128 pay for rows that are not there.
+static bool takes_many(const CacheDims& d, int rcap, bool f32) { return !f32 && (long long)rcap * d.G > 16; }
+
 }  // namespace ts
 
 using namespace ts;
 
 extern "C" size_t ts_tree_attention_workspace_bytes(const ts_ctx* ctx, const ts_cache_layout* lay, int32_t B) {
   if (!ctx || cache_layout_error(lay) || B < 1 || B > ctx->cfg.max_batch) return 0;
-  return attn_few_workspace(ctx, cache_dims(lay), lay->dtype == TS_DTYPE_F32);
+  const CacheDims d = cache_dims(lay);
+  const size_t few = attn_few_workspace(ctx, d, lay->dtype == TS_DTYPE_F32), many = attn_many_workspace(ctx, d);
+  return lay->dtype == TS_DTYPE_F32 || few > many ? few : many;
 }
 
 extern "C" int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* lay, int32_t B, const void* q, int64_t ldq, const void* pool,
@@ -542,7 +567,7 @@ extern "C" int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* lay, in
   a.qk = ldexpf(scale * LOG2E, K_SHIFT + lay->k_exp); a.vo = ldexpf(1.f, V_SHIFT + lay->v_exp);
   a.out = out; a.ldo = ldo; a.lse = lse; a.limit = ctx->wait_limit;
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e = attn_few_launch(ctx, a, f32, (char*)ws, st);
+  cudaError_t e = takes_many(a.d, a.rcap, f32) ? attn_many_launch(ctx, a, (char*)ws, st) : attn_few_launch(ctx, a, f32, (char*)ws, st);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? TS_OK : set_cuda_error("ts_tree_attention", e);
 }

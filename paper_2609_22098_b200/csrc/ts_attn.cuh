@@ -147,7 +147,13 @@ __device__ __forceinline__ float row_inv(float l) { return l == 0.f ? 0.f : 1.f 
 // what a part of a row counts in the whole; a part that has seen nothing counts zero (a NaN in it stays one)
 __device__ __forceinline__ float part_weight(float m, float top) { return m == -INFINITY ? 0.f : ex2(m - top); }
 
-size_t attn_few_workspace(const ts_ctx* ctx, const CacheDims& d, bool f32);
-cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, cudaStream_t st);
+// the workspace of a launch, and where its parts lie
+size_t attn_workspace(int grid, int QT, int Dh);
+void attn_place(AttnArgs& a, int QT, char* ws);
+cudaError_t attn_join(ts_ctx* ctx, const AttnArgs& a, int QT, bool f32, cudaStream_t st);
+// many query rows a kv head (ts_attn_many.cu), bf16 only
+cudaError_t attn_many_setup(ts_ctx* ctx);
+size_t attn_many_workspace(const ts_ctx* ctx, const CacheDims& d);
+cudaError_t attn_many_launch(ts_ctx* ctx, AttnArgs a, char* ws, cudaStream_t st);
 
 }  // namespace ts
