@@ -14,6 +14,7 @@ constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_BLOCKS = 2;                        // blocks a warp takes in a step: two score chains side by side
 constexpr int FEW_TOKENS = FEW_BLOCKS * CACHE_BLOCK;
+template <int NT> using FewShape = AttnShape<8 * NT, FEW_TOKENS, 1, 1>;
 
 template <int Dh, int NT>
 struct FewPlan {
@@ -57,7 +58,7 @@ struct Queries {
       const int idx = first + 8 * n + g;
       float x[Dh / 4];
       if (idx < u.rows * a.d.G) {
-        const size_t at = ((size_t)u.b * a.rcap + idx / a.d.G) * a.ldq + (size_t)(h * a.d.G + idx % a.d.G) * Dh + t * (Dh / 4);
+        const size_t at = head_row(a, u.b, h, idx, a.ldq) + t * (Dh / 4);
         if (F32) {
           const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + at);
 #pragma unroll
@@ -216,8 +217,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
   pdl_launch_dependents();
   AttnUnit u;
   long long start, end;
-  int active;
-  if (!attn_locate<QT, FEW_TOKENS, FEW_THREADS>(a, u, start, end, active)) return;
+  if (!attn_locate<FewShape<NT>, FEW_THREADS>(a, u, start, end)) return;
 
   // The copies run ahead of the arithmetic, across units: the warp's steps are w, w + 4, .. of the CTA's piece.  The cursor
   // stands at step fj of unit fu, in column fc and block fin of that page; the table's entries are read a step ahead.
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
     if (fj >= fu.n) {
       do {
         fj -= fu.n;
-        next_unit<QT, FEW_TOKENS>(a, fu);
+        next_unit<FewShape<NT>>(a, fu);
       } while (fj >= fu.n);
       fc = fj * FEW_BLOCKS / per; fin = fj * FEW_BLOCKS - fc * per; fh = fu.v / fu.nq;
     }
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
               const int rel = tok0 + k * CACHE_BLOCK + g + 8 * (c >> 1) - u.seq, idx = first + 8 * n + 2 * t + (c & 1);
-              const bool sees = ((here >> k) & 1) && (rel < 0 || row_sees(a, u.b, idx / a.d.G, rel, u.rows));
+              const bool sees = ((here >> k) & 1) && (rel < 0 || row_sees(a, u.b, tree_row(a, idx), rel, u.rows));
               if (!sees) s[k][n][c] = -INFINITY;
               if (!ok) s[k][n][c] = NAN;
             }
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
     }
     __syncthreads();
     pos += seg;
-    if (pos < steps) next_unit<QT, FEW_TOKENS>(a, u);
+    if (pos < steps) next_unit<FewShape<NT>>(a, u);
   }
   // after a wait that gave up copies may still be on their way into this CTA's memory
   if (gave_up)
@@ -564,6 +564,7 @@ extern "C" int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* lay, in
   a.d = cache_dims(lay);
   a.B = B; a.rcap = n_nodes ? ctx->cfg.Nmax + 1 : 1; a.N = ctx->cfg.Nmax; a.words = (ctx->cfg.Nmax + 63) / 64;
   a.q = q; a.ldq = ldq; a.pool = (const unsigned char*)pool; a.table = block_table; a.seq_len = seq_len; a.n_nodes = n_nodes; a.mask = mask;
+  a.by_g = (unsigned)(((1ull << 32) + a.d.G - 1) / a.d.G);   // (G = 1: not used)
   a.qk = ldexpf(scale * LOG2E, K_SHIFT + lay->k_exp); a.vo = ldexpf(1.f, V_SHIFT + lay->v_exp);
   a.out = out; a.ldo = ldo; a.lse = lse; a.limit = ctx->wait_limit;
   cudaStream_t st = (cudaStream_t)stream;

@@ -1,9 +1,10 @@
 // What the attention kernels over the 4-bit cache share: how the work is cut, who sees what, how pieces are joined.
 //
 // The work is a line of steps (a few blocks of one head for one tile of query rows): requests, then kv heads, then tiles of
-// rows, then steps.  A unit = the steps of one (request, head, tile).  The line is cut into equal pieces, one a CTA,
-// whatever the lengths are: lengths are known on the device only.  A unit that lies within one CTA is written by it; the
-// pieces of another go to the workspace, with a record by which the join kernel finds them.
+// rows, then steps.  A unit = the steps of one (request, head, tile).  A step is as long as its cost, and the line is cut
+// into equal pieces, one a CTA, whatever the lengths of the contexts are (they are known on the device only); a step belongs
+// to the piece in which it begins.  A unit that lies within one CTA is written by it; the pieces of another go to the
+// workspace, with a record by which the join kernel finds them.
 #pragma once
 
 #include "ts_cache.cuh"
@@ -19,6 +20,7 @@ struct AttnArgs {
   const unsigned char* pool;
   const int *table, *seq_len, *n_nodes;
   const uint64_t* mask;
+  unsigned by_g;           // ceil(2^32 / G): idx * by_g >> 32 = idx / G for all idx below 2^19 and G up to 1,024
   float qk, vo;            // powers of two of the operands, the scale and log2 e; what takes V's power of two back
   void* out; long long ldo;
   float* lse;
@@ -29,46 +31,59 @@ struct AttnArgs {
 };
 
 // pieces first..last of a unit; first < 0: nothing begins here that is to be joined
-struct AttnRecord { int b, v, first, last; long long t0; int nq, active; };
+struct AttnRecord { int b, v, first, last, nq; };
 
-struct AttnUnit { int b, v, n, nq, rows, seq; long long t0; };   // v = head * nq + tile; n steps, the first at place t0
+// v = head * nq + tile; n steps of length wt each, the first at place t0; wl: the length where a head's last tile is half full
+struct AttnUnit { int b, v, n, nq, rows, seq, wt, wl; long long t0; };
 
-// QT query rows a tile, TOK tokens a step
-template <int QT, int TOK>
-__device__ __forceinline__ long long unit_steps(const AttnArgs& a, int b, AttnUnit& u) {
+// QT query rows a tile, TOK tokens a step; a step is WIDE long, HALF where at most half of the tile's rows are there
+template <int QT_, int TOK_, int WIDE_, int HALF_>
+struct AttnShape {
+  static constexpr int QT = QT_, TOK = TOK_, WIDE = WIDE_, HALF = HALF_;
+};
+
+// the request's units: fills all of u but v, wt and t0; returns their length together
+template <class S>
+__device__ __forceinline__ long long unit_set(const AttnArgs& a, int b, AttnUnit& u) {
   u.b = b; u.seq = a.seq_len[b];
   u.rows = request_rows(a.n_nodes, b, a.rcap);
-  if (u.seq < 0) { u.n = 0; u.nq = 0; return 0; }
+  if (u.seq < 0) { u.n = 0; u.nq = 0; u.wl = 0; return 0; }
   const long long end = min((long long)u.seq + u.rows, (long long)a.d.cols * a.d.ps);   // (no page beyond the table's)
-  u.n = (int)max(1ll, (end + TOK - 1) / TOK);
-  u.nq = (u.rows * a.d.G + QT - 1) / QT;
-  return (long long)a.d.Hkv * u.nq * u.n;
+  u.n = (int)max(1ll, (end + S::TOK - 1) / S::TOK);
+  u.nq = (u.rows * a.d.G + S::QT - 1) / S::QT;
+  u.wl = u.rows * a.d.G - (u.nq - 1) * S::QT <= S::QT / 2 ? S::HALF : S::WIDE;
+  return (long long)a.d.Hkv * u.n * ((u.nq - 1) * S::WIDE + u.wl);
 }
+template <class S>
+__device__ __forceinline__ int unit_weight(const AttnUnit& u) { return S::WIDE == S::HALF ? S::WIDE : (u.v + 1) % u.nq == 0 ? u.wl : S::WIDE; }
 
-// CTAs that take part, and where piece c begins
-__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, total / a.min_steps)); }
+// CTAs that take part, where piece c begins, and the piece in which place x lies
+template <class S>
+__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, total / (a.min_steps * S::WIDE))); }
 __device__ __forceinline__ long long piece_start(long long total, int active, int c) { return total * c / active; }
+__device__ __forceinline__ int piece_of(long long total, int active, long long x) { return (int)(((x + 1) * active + total - 1) / total) - 1; }
 
-template <int QT, int TOK>
+template <class S>
 __device__ __forceinline__ void next_unit(const AttnArgs& a, AttnUnit& u) {
-  u.t0 += u.n;
-  if (++u.v < a.d.Hkv * u.nq) return;
-  u.v = 0;
-  while (++u.b < a.B) {
-    AttnUnit n = u;
-    if (unit_steps<QT, TOK>(a, u.b, n) > 0) { n.t0 = u.t0; n.v = 0; u = n; return; }
+  u.t0 += (long long)u.n * u.wt;
+  if (++u.v >= a.d.Hkv * u.nq) {
+    u.v = 0;
+    for (int b = u.b + 1; b < a.B; ++b)
+      if (unit_set<S>(a, b, u) > 0) break;
   }
+  u.wt = unit_weight<S>(u);
 }
 
-// Finds the whole line's length and the unit in which this CTA's piece begins.  All threads call it; false: no piece.
-template <int QT, int TOK, int THREADS>
-__device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, long long& end, int& active) {
+// Finds the unit in which this CTA's first step lies, the place of that step and the end of the piece.  All threads call it;
+// false: no step.
+template <class S, int THREADS>
+__device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, long long& end) {
   __shared__ long long wsum[THREADS / 32];
   __shared__ AttnUnit found;
   const int per = (a.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   AttnUnit n;
   long long sum = 0;
-  for (int b = b0; b < min(b0 + per, a.B); ++b) sum += unit_steps<QT, TOK>(a, b, n);
+  for (int b = b0; b < min(b0 + per, a.B); ++b) sum += unit_set<S>(a, b, n);
   long long inc = sum;
   for (int o = 1; o < 32; o <<= 1) {
     const long long v = __shfl_up_sync(~0u, inc, o);
@@ -81,20 +96,22 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, lo
     if (w < warp) before += wsum[w];
     total += wsum[w];
   }
-  active = attn_active(a, total);
+  const int active = attn_active<S>(a, total);
   if (total == 0 || (int)blockIdx.x >= active) {
     if (threadIdx.x == 0) a.records[blockIdx.x].first = -1;
     return false;
   }
-  start = piece_start(total, active, blockIdx.x);
+  const long long x0 = piece_start(total, active, blockIdx.x);
   end = piece_start(total, active, blockIdx.x + 1);
   long long at = before + inc - sum;
-  if (start >= at && start < at + sum)
+  if (x0 >= at && x0 < at + sum)
     for (int b = b0;; ++b) {
-      const long long w = unit_steps<QT, TOK>(a, b, n);
-      if (start < at + w) {
-        n.v = (int)((start - at) / n.n);
-        n.t0 = at + (long long)n.v * n.n;
+      const long long w = unit_set<S>(a, b, n);
+      if (x0 < at + w) {
+        const long long head = w / a.d.Hkv, x = x0 - at, h = x / head, q = min((x - h * head) / ((long long)n.n * S::WIDE), (long long)n.nq - 1);
+        n.v = (int)(h * n.nq + q);
+        n.t0 = at + h * head + q * n.n * S::WIDE;
+        n.wt = unit_weight<S>(n);
         found = n;
         break;
       }
@@ -102,16 +119,20 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, lo
     }
   __syncthreads();
   u = found;
+  long long j = (x0 - u.t0 + u.wt - 1) / u.wt;
+  if (j >= u.n && u.t0 + (long long)u.n * u.wt < total) { next_unit<S>(a, u); j = 0; }
+  start = u.t0 + j * u.wt;
+  const bool any = j < u.n && start < end;
   if (threadIdx.x == 0) {
     // the first cut within the unit: the piece before this one holds its beginning
-    AttnRecord r{u.b, u.v, -1, 0, u.t0, u.nq, active};
-    if (start > u.t0 && piece_start(total, active, blockIdx.x - 1) <= u.t0) {
+    AttnRecord r{u.b, u.v, -1, 0, u.nq};
+    if (any && j > 0 && piece_of(total, active, u.t0) == (int)blockIdx.x - 1) {
       r.first = blockIdx.x - 1;
-      r.last = (int)(((u.t0 + u.n) * active + total - 1) / total) - 1;   // the last c with start(c) < end of the unit
+      r.last = piece_of(total, active, u.t0 + (long long)(u.n - 1) * u.wt);
     }
     a.records[blockIdx.x] = r;
   }
-  return true;
+  return any;
 }
 
 // Whether tree row i of request b sees the token at place rel behind the prefix (rel >= 0).
@@ -137,9 +158,17 @@ __device__ __forceinline__ float lg2(float x) {
 __device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_out(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 
-// where row idx of a request's head goes
-__device__ __forceinline__ size_t out_row(const AttnArgs& a, int b, int h, int idx) { return ((size_t)b * a.rcap + idx / a.d.G) * a.ldo + (size_t)(h * a.d.G + idx % a.d.G) * a.d.Dh; }
-__device__ __forceinline__ size_t lse_row(const AttnArgs& a, int b, int h, int idx) { return ((size_t)b * a.rcap + idx / a.d.G) * a.d.Hq + h * a.d.G + idx % a.d.G; }
+// the tree row of row idx of a kv head, and where that row goes
+__device__ __forceinline__ int tree_row(const AttnArgs& a, int idx) { return a.d.G == 1 ? idx : (int)__umulhi((unsigned)idx, a.by_g); }
+__device__ __forceinline__ size_t head_row(const AttnArgs& a, int b, int h, int idx, long long ld) {
+  const int i = tree_row(a, idx);
+  return ((size_t)b * a.rcap + i) * ld + (size_t)(h * a.d.G + idx - i * a.d.G) * a.d.Dh;
+}
+__device__ __forceinline__ size_t out_row(const AttnArgs& a, int b, int h, int idx) { return head_row(a, b, h, idx, a.ldo); }
+__device__ __forceinline__ size_t lse_row(const AttnArgs& a, int b, int h, int idx) {
+  const int i = tree_row(a, idx);
+  return ((size_t)b * a.rcap + i) * a.d.Hq + h * a.d.G + idx - i * a.d.G;
+}
 
 // A row's weight sum l relative to 2^m, as the natural logarithm of the row's sum.  No token: l = 0.
 __device__ __forceinline__ float row_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + lg2(l)) * LN2; }

@@ -2,12 +2,15 @@
 //
 // One CTA an SM with a piece of the line of steps (128 tokens of one head).  Roles:
 //   loader        one warp: bulk copies of the cache's blocks into a ring of 64 tokens a stage
-//   converters    eight warps: codes to fp16 (exact) in the operands' swizzled layout, K and V two stages each
-//   issuer        one warp: S = Q K^T (128 rows x 128 tokens) and O += P V, accumulators and P in tensor memory
-//   softmax       two groups of four warps, a thread a query row: scores to weights in place, fp16
+//   converters    two warps for K, two for V: codes to fp16 (exact) in the operands' swizzled layout, two stages each
+//   issuer        one thread: S = Q K^T (128 rows x 128 tokens) and O += P V, accumulators and P in tensor memory
+//   softmax       two groups of eight warps, two threads a query row with 64 of a step's scores each: scores to weights in
+//                 place, fp16.  (With one thread a row a step's scores took it 2,500 cycles, which its next product waited for.)
 // A unit has up to 256 query rows.  With more than 128 the groups take a tile of 128 rows each, and both read the same
 // converted keys and values; with fewer they take the same rows and every other step, and their halves are joined at the end.
 // Either way one group's exponentials run beside the other's matrix products.
+#include <string.h>
+
 #include "ts_attn.cuh"
 #include "ts_tc.cuh"
 
@@ -15,7 +18,10 @@ namespace ts {
 
 constexpr int MANY_TOKENS = 128;                  // a step
 constexpr int MANY_QT = 256;
-constexpr int MANY_SOFT = 8, MANY_CONV = 8;       // warps
+// A step with one tile of rows costs this share of one with two (measured on 16,000 tokens a unit; both sides in DESIGN).
+using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 5, 3>;
+constexpr int MANY_SOFT = 16, MANY_CONV = 4;      // warps (converters: half for K, half for V)
+constexpr int MANY_CT = MANY_CONV / 2 * 32;       // threads of either kind
 constexpr int MANY_ISSUE = MANY_SOFT + MANY_CONV, MANY_LOAD = MANY_ISSUE + 1, MANY_WARPS = MANY_LOAD + 1;
 constexpr int MANY_THREADS = MANY_WARPS * 32;
 constexpr int MANY_RAW = 3;                       // stages of raw blocks
@@ -29,17 +35,15 @@ struct ManyPlan {
   static constexpr int RAW = MANY_RAW_BLOCKS * cache_block_bytes(Dh);
   static constexpr int Q = 0, K = 2 * TILE, V = 4 * TILE, R = 6 * TILE;
   static constexpr int SMEM = 6 * TILE + MANY_RAW * RAW + 1024;   // (the dynamic array is aligned to 1,024 in the kernel)
-  static constexpr uint32_t O = 256;              // tensor memory columns: S of the groups at 0 and 128, P in their first 64
+  static constexpr uint32_t O = 256;              // tensor memory columns: S of the groups at 0 and 128; P of 64 tokens in the first 32 columns of their scores
 };
 
 struct ManyBars {
   uint64_t raw_full[MANY_RAW], raw_free[MANY_RAW];
-  uint64_t k_full[2], k_free[2], v_full[2], v_free[2];
-  uint64_t q_full, s_full[2], p_full[2], o_full[2];
+  uint64_t k_full[2], v_full[2], k_free[2][2], v_free[2][2];   // (free: by group and stage)
+  uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
 };
 
-// D = f32, A = B = f16, M = 128, N = n; B MN-major (values) or K-major (keys)
-__device__ __forceinline__ uint32_t many_idesc(int n, bool mn_major) { return (1u << 4) | (mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24); }
 __device__ __forceinline__ void mma_tmem_a(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -56,232 +60,318 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
       : "r"(taddr) : "memory");
 }
 #undef TS_R4
+// the wait, with the registers that it waits for: nothing that uses them can be moved before it
+#define TS_B4(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3])
+__device__ __forceinline__ void tmem_ld32_wait(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : TS_B4(r, 0), TS_B4(r, 4), TS_B4(r, 8), TS_B4(r, 12), TS_B4(r, 16), TS_B4(r, 20), TS_B4(r, 24), TS_B4(r, 28)::"memory");
+}
+__device__ __forceinline__ void tmem_ld16_wait(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : TS_B4(r, 0), TS_B4(r, 4), TS_B4(r, 8), TS_B4(r, 12)::"memory");
+}
+#undef TS_B4
 #define TS_W4(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3])
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
                ::TS_W4(r, 0), TS_W4(r, 4), TS_W4(r, 8), TS_W4(r, 12), "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, "
-      "%29, %30, %31};"
-      ::TS_W4(r, 0), TS_W4(r, 4), TS_W4(r, 8), TS_W4(r, 12), TS_W4(r, 16), TS_W4(r, 20), TS_W4(r, 24), TS_W4(r, 28), "r"(taddr) : "memory");
-}
 #undef TS_W4
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// all softmax warps; the two that share 32 rows
+__device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(MANY_SOFT * 32) : "memory"); }
+__device__ __forceinline__ void pair_sync(int quad) { asm volatile("bar.sync %0, 64;" ::"r"(2 + quad) : "memory"); }
+
+// where a CTA's piece begins and ends
+struct ManyPiece { AttnUnit u; long long start, end; };
 
 struct ManyShared {
+  ManyPiece piece;
   ManyBars bars;
   uint32_t tmem;
   int abort;
   unsigned char present[MANY_PRESENT];   // a bit for each block of a step
-  float ml[2][128][2];                   // reference and sum of the two groups, where they share rows
+  float top[2][2][128];                  // largest scores of a step, by group and half
+  float ml[2][2][128][2];                // reference and sum of a row, by group and half
 };
 
+// Every role reads its own copy of the piece: kept in registers across the parting of the roles it was spilled in all of them.
+__device__ __forceinline__ ManyPiece my_piece(const ManyShared& sh) {
+  ManyPiece p;
+  constexpr int W = sizeof(ManyPiece) / 4;
+  static_assert(sizeof(ManyPiece) % 4 == 0, "words");
+  uint32_t w[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const volatile uint32_t*>(&sh.piece)[i];
+  memcpy(&p, w, sizeof(p));
+  return p;
+}
+
 // The steps of a CTA's piece that belong to one unit.
-struct ManySegment { int h, first, j0, n, two; bool whole; };
-template <int Dh>
-__device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const AttnUnit& u, long long start, long long end, long long at) {
+struct ManySegment { int h, first, j0, n, two; bool whole; long long next; };
+__device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const AttnUnit& u, long long at, long long end) {
   ManySegment s;
   s.h = u.v / u.nq;
   s.first = (u.v - s.h * u.nq) * MANY_QT;
-  s.j0 = (int)(at - u.t0);
-  s.n = (int)min((long long)(u.n - s.j0), end - at);
+  s.j0 = (int)(at - u.t0) / u.wt;   // (a unit has less than 2^24 steps)
+  s.n = min(u.n - s.j0, (int)(min(end - at, 1ll << 30) + u.wt - 1) / u.wt);
+  s.next = at + (long long)s.n * u.wt;
   s.two = u.rows * a.d.G - s.first > 128;
   s.whole = s.n == u.n;
   return s;
 }
 
-// ---- loader -------------------------------------------------------------------------------------------------------------
-template <int Dh>
-__device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw, AttnUnit u, long long start, long long end) {
-  using P = ManyPlan<Dh>;
-  const int lane = threadIdx.x & 31, per = a.d.ps / CACHE_BLOCK, half_steps = (int)(end - start) * 2;
-  long long at = start;
-  int page = -1, inner = 0, h = u.v / u.nq;
-  // entry of the table for this lane's block of half-step `hs`
-  auto look_up = [&](int hs) {
-    if (hs >= half_steps) return;
-    const long long p = start + (hs >> 1);
-    while (p >= u.t0 + u.n) { next_unit<MANY_QT, MANY_TOKENS>(a, u); h = u.v / u.nq; }
-    const int jb = (int)(p - u.t0) * (MANY_TOKENS / CACHE_BLOCK) + (hs & 1) * MANY_RAW_BLOCKS + lane, c = jb / per;
-    inner = jb - c * per;
-    const unsigned last = (unsigned)u.seq + (unsigned)u.rows - 1u;
-    page = lane < MANY_RAW_BLOCKS && c < a.d.cols && (unsigned)jb * CACHE_BLOCK <= last ? __ldg(a.table + (size_t)u.b * a.d.cols + c) : -1;
-  };
-  look_up(0);
-  int slot = 0;
-  uint32_t phase = 0, seen = 0;
-  for (int hs = 0; hs < half_steps; ++hs) {
-    const long long off = block_offset(a.d, page, inner, h);
-    const unsigned there = __ballot_sync(~0u, off >= 0);
-    look_up(hs + 1);
-    if (hs >= MANY_RAW && !__all_sync(~0u, mbar_wait(&sh.bars.raw_free[slot], phase ^ 1u, (volatile int*)&sh.abort, nullptr, a.limit))) break;
-    if (lane == 0) {
-      unsigned char* pr = &sh.present[(hs >> 1) % MANY_PRESENT];
-      *pr = (unsigned char)((hs & 1) ? *pr | there << 4 : there);
-      mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * cache_block_bytes(Dh));
-    }
-    __syncwarp();
-    if (off >= 0)
-      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                   ::"r"(smem_u32(raw + slot * P::RAW + lane * cache_block_bytes(Dh))), "l"(a.pool + off), "r"((uint32_t)cache_block_bytes(Dh)), "r"(smem_u32(&sh.bars.raw_full[slot])) : "memory");
-    __syncwarp();
-    seen |= 1u << slot;
-    if (++slot == MANY_RAW) { slot = 0; phase ^= 1u; }
+// The steps of a CTA's piece, unit by unit.
+__device__ __forceinline__ int many_steps(const AttnArgs& a, AttnUnit u, long long at, long long end) {
+  int n = 0;
+  while (at < end) {
+    const ManySegment s = many_segment(a, u, at, end);
+    n += s.n;
+    at = s.next;
+    if (at < end) next_unit<ManyShape>(a, u);
   }
-  // after a wait that gave up copies may still be on their way: (the last use of a slot completes the phase before the next)
+  return n;
+}
+
+// ---- loader -------------------------------------------------------------------------------------------------------------
+// The warp's lanes have a block each of four steps: looked up in the table together, asked for in L2 at once, and copied one
+// batch later, half a step at a time.  (The ring alone has room for 27 KB on their way, less than memory needs; and one look-up
+// after the other took longer than a step.)
+template <int Dh>
+__device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw) {
+  using P = ManyPlan<Dh>;
+  const ManyPiece piece = my_piece(sh);
+  AttnUnit u = piece.u;
+  const long long start = piece.start, end = piece.end;
+  constexpr uint32_t BLK = cache_block_bytes(Dh);
+  const int lane = threadIdx.x & 31, per = a.d.ps / CACHE_BLOCK, half_steps = 2 * many_steps(a, u, start, end);
+  int j = (int)(start - u.t0) / u.wt + (lane >> 3), mine = lane >> 2;   // the lane's step within its unit, its half-step in all
+  int page = -1, inner = 0;
+  auto look_up = [&]() {
+    page = -1;
+    if (mine >= half_steps) return;
+    while (j >= u.n) { j -= u.n; next_unit<ManyShape>(a, u); }
+    const int jb = j * (MANY_TOKENS / CACHE_BLOCK) + (lane & 7), c = jb / per;
+    inner = jb - c * per;
+    const unsigned last = (unsigned)u.seq + (unsigned)u.rows - 1u;   // the request's last token; a block behind it is not fetched
+    if (c < a.d.cols && (unsigned)jb * CACHE_BLOCK <= last) page = __ldg(a.table + (size_t)u.b * a.d.cols + c);
+  };
+  auto place = [&]() {
+    const long long off = block_offset(a.d, page, inner, u.v / u.nq);
+    if (off >= 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.pool + off), "r"(BLK) : "memory");
+    mine += 8; j += 4;
+    return off;
+  };
+  look_up();
+  long long now = place();
+  int slot = 0, copied = 0;
+  uint32_t phase = 0;
+  bool alive = true;
+  while (copied < half_steps && alive) {
+    look_up();                       // the next batch's entries are on their way while this one is copied
+    const unsigned there8 = __ballot_sync(~0u, now >= 0);
+    for (int k = 0; k < 8 && copied < half_steps; ++k, ++copied) {
+      const unsigned there = there8 >> (4 * k) & 0xFu;
+      if (copied >= MANY_RAW && !__all_sync(~0u, mbar_wait(&sh.bars.raw_free[slot], phase ^ 1u, (volatile int*)&sh.abort, nullptr, a.limit))) { alive = false; break; }
+      if (lane == 0) {
+        unsigned char* pr = &sh.present[(copied >> 1) % MANY_PRESENT];
+        *pr = (unsigned char)((copied & 1) ? *pr | there << 4 : there);
+        mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * BLK);
+      }
+      __syncwarp();
+      if (lane >> 2 == k && now >= 0)
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     ::"r"(smem_u32(raw + slot * P::RAW + (lane & 3) * BLK)), "l"(a.pool + now), "r"(BLK), "r"(smem_u32(&sh.bars.raw_full[slot])) : "memory");
+      __syncwarp();
+      if (++slot == MANY_RAW) { slot = 0; phase ^= 1u; }
+    }
+    now = place();
+  }
+  // after a wait that gave up copies may still be on their way (the last use of a slot completes the phase before the next)
   if (sh.abort)
-    for (int s = 0; s < MANY_RAW; ++s)
-      if (seen >> s & 1u)
-        for (uint32_t i = 0; i < a.limit && !mbar_try_wait(&sh.bars.raw_full[s], s < slot ? phase : phase ^ 1u); ++i) __nanosleep(100);
+    for (int s = 0; s < MANY_RAW && s < copied; ++s)
+      for (uint32_t i = 0; i < a.limit && !mbar_try_wait(&sh.bars.raw_full[s], s < slot ? phase : phase ^ 1u); ++i) __nanosleep(100);
 }
 
 // ---- converters ---------------------------------------------------------------------------------------------------------
-// K [token][channel], K-major: rows of 64 channels (128 bytes), 16-byte chunks exchanged by the row's last three bits.
+// A thread's part of 64 raw tokens.  It is read at once, so that the ring's slot is free again before anything is converted.
+// K: Dh/8 bytes of the codes of two tokens, with their scales.
 template <int Dh>
-__device__ __forceinline__ void convert_keys(const unsigned char* raw, unsigned char* dst, int half, int tid) {
-  // a thread: 64 bytes of results, Dh/8 bytes of a token's codes (Dh = 128: 32 channels; 64: 16)
-  const int tok = tid >> 2, q = tid & 3, row = half * 64 + tok;
-  const unsigned char* blk = raw + (tok >> 4) * cache_block_bytes(Dh);
-  const unsigned char* sp = blk + off_ks(Dh) + (tok & 15) * (Dh / CACHE_GROUP) + q * (Dh / 64);
-  constexpr int W = Dh / 32;
-  uint32_t w[W];
-  __half2 sc;
-  int turn = 0;
-  if (Dh == 128) {
-    const uint4 v = *reinterpret_cast<const uint4*>(blk + (tok & 15) * (Dh / 2) + q * 16);
-    sc = k_scales(*reinterpret_cast<const unsigned short*>(sp));
-    // lanes of the two halves of a row write to other banks: the second pair of words first
-    turn = q & 2;
-    w[0] = turn ? v.z : v.x; w[1] = turn ? v.w : v.y; w[W - 2] = turn ? v.x : v.z; w[W - 1] = turn ? v.y : v.w;
-    if (turn) sc = __lowhigh2highlow(sc);
-  } else {
-    const uint2 v = *reinterpret_cast<const uint2*>(blk + (tok & 15) * (Dh / 2) + q * 8);
-    w[0] = v.x; w[1] = v.y;
-    sc = k_scales(*sp);
-  }
+struct KeyPart {
+  static constexpr int W = Dh / 32, N = 256 / MANY_CT;
+  uint32_t k[N][W], s[N];
+  __device__ __forceinline__ void read(const unsigned char* raw, int tid) {
 #pragma unroll
-  for (int i = 0; i < W; ++i) {
-    const __half2 ss = Dh == 128 && i >= W / 2 ? __high2half2(sc) : __low2half2(sc);
-    uint32_t x[4];
-    unpack8(w[i], ss, __hmul2(ss, __float2half2_rn(-1032.f)), __hmul2(ss, __float2half2_rn(-72.f)), x);
-    const int chunk = q * W + (i ^ turn);   // of eight channels
-    *reinterpret_cast<uint4*>(dst + (chunk >> 3) * ManyPlan<Dh>::SLAB + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+    for (int n = 0; n < N; ++n) {
+      const int tok = (tid >> 2) + n * (MANY_CT / 4), q = tid & 3;
+      const unsigned char* blk = raw + (tok >> 4) * cache_block_bytes(Dh);
+      const unsigned char* sp = blk + off_ks(Dh) + (tok & 15) * (Dh / CACHE_GROUP) + q * (Dh / 64);
+      if (Dh == 128) {
+        const uint4 x = *reinterpret_cast<const uint4*>(blk + (tok & 15) * (Dh / 2) + q * 16);
+        k[n][0] = x.x; k[n][1] = x.y; k[n][W - 2] = x.z; k[n][W - 1] = x.w;
+        s[n] = *reinterpret_cast<const unsigned short*>(sp);
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(blk + (tok & 15) * (Dh / 2) + q * 8);
+        k[n][0] = x.x; k[n][1] = x.y;
+        s[n] = *sp;
+      }
+    }
   }
-}
-// V [token][channel], MN-major: the same rows; tokens are the contraction.
-template <int Dh>
-__device__ __forceinline__ void convert_values(const unsigned char* raw, unsigned char* dst, int half, int tid) {
+  // [token][channel], K-major: rows of 64 channels (128 bytes), 16-byte chunks exchanged by the row's last three bits
+  __device__ __forceinline__ void write(unsigned char* dst, int half, int tid) const {
 #pragma unroll
-  for (int k = 0; k < Dh / 64; ++k) {
-    const int item = tid + k * (MANY_CONV * 32);               // [block][octet][group][token]
-    const int t8 = item & 7, rest = item >> 3, g = rest % (Dh / CACHE_GROUP), oct = rest / (Dh / CACHE_GROUP), row = half * 64 + oct * 8 + t8;
-    const unsigned char* blk = raw + (oct >> 1) * cache_block_bytes(Dh);
-    const uint2 w = *reinterpret_cast<const uint2*>(blk + off_vc(Dh) + (oct & 1) * (4 * Dh) + g * 64 + t8 * 8);
-    const uint32_t byte = blk[off_vs(Dh) + (oct & 1) * (Dh / 2) + g * 8 + t8];
-    const __half2 ss = v_scales(byte * 0x101u), c1032 = __hmul2(ss, __float2half2_rn(-1032.f)), c72 = __hmul2(ss, __float2half2_rn(-72.f));
-    unsigned char* out = dst + (g >> 2) * ManyPlan<Dh>::SLAB + row * 128;
-    uint32_t x[4];
-    unpack8(w.x, ss, c1032, c72, x);
-    *reinterpret_cast<uint4*>(out + ((((g & 3) * 2) ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
-    unpack8(w.y, ss, c1032, c72, x);
-    *reinterpret_cast<uint4*>(out + ((((g & 3) * 2 + 1) ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+    for (int n = 0; n < N; ++n) {
+      const int row = half * 64 + (tid >> 2) + n * (MANY_CT / 4), q = tid & 3, turn = Dh == 128 ? q & 2 : 0;
+      const __half2 both = k_scales(s[n]), sc = turn ? __lowhigh2highlow(both) : both;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        // (lanes of the two halves of a row would write to the same banks: those of the second take their words in another order)
+        const uint32_t w = turn ? k[n][(i + 2) % W] : k[n][i];
+        const __half2 ss = Dh == 128 && i >= W / 2 ? __high2half2(sc) : __low2half2(sc);
+        uint32_t x[4];
+        unpack8(w, ss, __hmul2(ss, __float2half2_rn(-1032.f)), __hmul2(ss, __float2half2_rn(-72.f)), x);
+        const int chunk = q * W + (i ^ turn);   // of eight channels
+        *reinterpret_cast<uint4*>(dst + (chunk >> 3) * ManyPlan<Dh>::SLAB + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+      }
+    }
   }
-}
+};
+// V: eight bytes of codes (a group of 16 channels) of Dh/32 tokens, with their scales.
 template <int Dh>
-__device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* smem, int steps) {
+struct ValuePart {
+  static constexpr int N = 64 * (Dh / CACHE_GROUP) / MANY_CT;
+  uint2 v[N]; uint32_t s[N];
+  // item: [octet][group][token]
+  static __device__ __forceinline__ void item(int tid, int n, int& oct, int& g, int& t8) {
+    const int e = tid + n * MANY_CT;
+    t8 = e & 7; g = (e >> 3) % (Dh / CACHE_GROUP); oct = (e >> 3) / (Dh / CACHE_GROUP);
+  }
+  __device__ __forceinline__ void read(const unsigned char* raw, int tid) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      int oct, g, t8;
+      item(tid, n, oct, g, t8);
+      const unsigned char* b = raw + (oct >> 1) * cache_block_bytes(Dh);
+      v[n] = *reinterpret_cast<const uint2*>(b + off_vc(Dh) + (oct & 1) * (4 * Dh) + g * 64 + t8 * 8);
+      s[n] = b[off_vs(Dh) + (oct & 1) * (Dh / 2) + g * 8 + t8];
+    }
+  }
+  // [token][channel], MN-major: the same rows; tokens are the contraction
+  __device__ __forceinline__ void write(unsigned char* dst, int half, int tid) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      int oct, g, t8;
+      item(tid, n, oct, g, t8);
+      const int row = half * 64 + oct * 8 + t8;
+      const __half2 ss = v_scales(s[n] * 0x101u), c1032 = __hmul2(ss, __float2half2_rn(-1032.f)), c72 = __hmul2(ss, __float2half2_rn(-72.f));
+      unsigned char* out = dst + (g >> 2) * ManyPlan<Dh>::SLAB + row * 128;
+      uint32_t x[4];
+      unpack8(v[n].x, ss, c1032, c72, x);
+      *reinterpret_cast<uint4*>(out + ((((g & 3) * 2) ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+      unpack8(v[n].y, ss, c1032, c72, x);
+      *reinterpret_cast<uint4*>(out + ((((g & 3) * 2 + 1) ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+    }
+  }
+};
+// One operand's converters: Part reads and writes it, `full` and `free` are its barriers.
+template <class Part, int Dh>
+__device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* raw, unsigned char* stages, uint64_t* full, uint64_t (*free)[2], int tid) {
   using P = ManyPlan<Dh>;
-  const int tid = threadIdx.x - MANY_SOFT * 32, lane = threadIdx.x & 31;
+  const ManyPiece piece = my_piece(sh);
+  AttnUnit u = piece.u;
+  const long long end = piece.end;
+  const int lane = threadIdx.x & 31;
   volatile int* abort = (volatile int*)&sh.abort;
-  int slot = 0;
+  int slot = 0, gj = 0;
   uint32_t phase = 0;
-  for (int j = 0; j < steps; ++j) {
-    const int st = j & 1;
-    const uint32_t par = ((uint32_t)(j >> 1) & 1u) ^ 1u;   // of the use before
-    unsigned char *k = smem + P::K + st * P::TILE, *v = smem + P::V + st * P::TILE;
-    int s2 = slot;
-    uint32_t p2 = phase;
-    if (j >= 2 && !mbar_wait(&sh.bars.k_free[st], par, abort, nullptr, a.limit)) return;
+  uint32_t used = 0;   // who read the stages last: bits of groups, by stage
+  uint32_t turn = 0;   // parity of the uses so far, a bit for each group and stage
+  for (long long at = piece.start; at < end;) {
+    const ManySegment s = many_segment(a, u, at, end);
+#pragma unroll 1
+    for (int j = 0; j < s.n; ++j, ++gj) {
+      const int st = gj & 1;
+      const uint32_t before = used >> (2 * st) & 3u;
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        Part part;
+        if (!mbar_wait(&sh.bars.raw_full[slot], phase, abort, nullptr, a.limit)) return;
+        part.read(raw + slot * P::RAW, tid);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.bars.raw_free[slot]);
+        if (++slot == MANY_RAW) { slot = 0; phase ^= 1u; }
+        if (half == 0) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      if (!mbar_wait(&sh.bars.raw_full[s2], p2, abort, nullptr, a.limit)) return;
-      convert_keys<Dh>(smem + P::R + s2 * P::RAW, k, half, tid);
-      if (++s2 == MANY_RAW) { s2 = 0; p2 ^= 1u; }
-    }
-    fence_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.bars.k_full[st]);
-    if (j >= 2 && !mbar_wait(&sh.bars.v_free[st], par, abort, nullptr, a.limit)) return;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      convert_values<Dh>(smem + P::R + slot * P::RAW, v, half, tid);
+          for (int g = 0; g < 2; ++g)
+            if (before >> g & 1u && !mbar_wait(&free[g][st], (turn >> (2 * st + g) & 1u) ^ 1u, abort, nullptr, a.limit)) return;
+        }
+        part.write(stages + st * P::TILE, half, tid);
+      }
+      fence_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.bars.raw_free[slot]);
-      if (++slot == MANY_RAW) { slot = 0; phase ^= 1u; }
+      if (lane == 0) mbar_arrive(&full[st]);
+      const uint32_t by = s.two ? 3u : 1u << (j & 1);
+      used = (used & ~(3u << (2 * st))) | by << (2 * st);
+      turn ^= by << (2 * st);
     }
-    fence_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.bars.v_full[st]);
+    at = s.next;
+    if (at < end) next_unit<ManyShape>(a, u);
   }
 }
 
 // ---- issuer -------------------------------------------------------------------------------------------------------------
+// One thread.  (Tensor memory begins at column 0: all of it is allocated.)  The groups' products are issued in turn, so that
+// one group's run while the other has its scores: issued by a thread each they fall into step, and tensor cores and exponentials
+// wait for one another.
 template <int Dh>
-__device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* smem, AttnUnit u, long long start, long long end) {
+__device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* smem) {
   using P = ManyPlan<Dh>;
+  const ManyPiece piece = my_piece(sh);
+  AttnUnit u = piece.u;
+  const long long end = piece.end;
   volatile int* abort = (volatile int*)&sh.abort;
-  const uint32_t tmem = sh.tmem, id_s = many_idesc(MANY_TOKENS, false), id_o = many_idesc(Dh, true);
+  constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(MANY_TOKENS >> 3) << 17) | ((128u >> 4) << 24);              // D = f32, A = B = f16, M = 128; B K-major: keys
+  constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(Dh >> 3) << 17) | ((128u >> 4) << 24);          // B MN-major: values
   const uint64_t qd = smem_desc(smem_u32(smem + P::Q), 16u, 1024u), kd = smem_desc(smem_u32(smem + P::K), 16u, 1024u), vd = smem_desc(smem_u32(smem + P::V), P::SLAB, 1024u);
-  uint32_t p_count[2] = {0u, 0u};   // weights waited for, per group
-  int base = 0, segments = 0;       // steps before this segment
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(~0u, mbar_wait(bar, parity, abort, nullptr, a.limit)); };
-  for (long long at = start; at < end;) {
-    const ManySegment s = many_segment<Dh>(a, u, start, end, at);
+  uint32_t weights = 0, segments = 0;   // weights: parity of the waits for each group's
+  int base = 0;                         // steps before this segment
+  for (long long at = piece.start; at < end; ++segments) {
+    const ManySegment s = many_segment(a, u, at, end);
     const int ops = s.two ? 2 * s.n : s.n;
-    if (!wait(&sh.bars.q_full, segments & 1)) return;
     // product i: group i & 1, step i / 2 (two tiles) or i; its P V is issued two products later
+#pragma unroll 1
     for (int i = 0; i < ops + 2; ++i) {
-      const int tile = i & 1;
+      const int g = i & 1;
       if (i >= 2) {
-        const int j = s.two ? (i - 2) >> 1 : i - 2, gj = base + j;
-        if (!wait(&sh.bars.p_full[tile], p_count[tile] & 1u)) return;
-        ++p_count[tile];
-        if (!wait(&sh.bars.v_full[gj & 1], (gj >> 1) & 1)) return;
+        const int gj = base + (s.two ? (i - 2) >> 1 : i - 2), st = gj & 1;
+        if (!mbar_wait(&sh.bars.p_full[g], weights >> g & 1u, abort, nullptr, a.limit)) return;
+        weights ^= 1u << g;
+        if (!mbar_wait(&sh.bars.v_full[st], (gj >> 1) & 1u, abort, nullptr, a.limit)) return;
         tc_fence_after();
-        if (elect_one()) {
-          const uint32_t d = tmem + P::O + tile * Dh, pa = tmem + tile * 128;
-          const uint64_t b = vd + (uint64_t)((gj & 1) * (P::TILE >> 4));
-          const uint32_t fresh = i < 4 ? 0u : 1u;   // the group's first of the unit
+        const uint64_t b = vd + (uint64_t)(st * (P::TILE >> 4));
+        const uint32_t more = i >= 4 ? 1u : 0u, o_at = P::O + g * Dh, s_at = g * 128;
 #pragma unroll
-          for (int ks = 0; ks < MANY_TOKENS / 16; ++ks) mma_tmem_a(d, pa + ks * 8, b + (uint64_t)(ks * 128), id_o, ks > 0 ? 1u : fresh);
-          mma_commit(&sh.bars.o_full[tile]);
-          if (!s.two || tile == 1) mma_commit(&sh.bars.v_free[gj & 1]);
-        }
-        __syncwarp();
+        for (int ks = 0; ks < MANY_TOKENS / 16; ++ks) mma_tmem_a(o_at, s_at + (ks >> 2) * 64 + (ks & 3) * 8, b + (uint64_t)(ks * 128), id_o, ks > 0 ? 1u : more);
+        mma_commit(&sh.bars.o_full[g]);
+        mma_commit(&sh.bars.v_free[g][st]);
       }
       if (i < ops) {
-        const int j = s.two ? i >> 1 : i, gj = base + j;
-        if (!wait(&sh.bars.k_full[gj & 1], (gj >> 1) & 1)) return;
+        const int gj = base + (s.two ? i >> 1 : i), st = gj & 1;
+        if (i < 2 && !mbar_wait(&sh.bars.q_full[g], segments & 1u, abort, nullptr, a.limit)) return;
+        if (!mbar_wait(&sh.bars.k_full[st], (gj >> 1) & 1u, abort, nullptr, a.limit)) return;
         tc_fence_after();
-        if (elect_one()) {
-          const uint64_t qa = qd + (uint64_t)((s.two ? tile : 0) * (P::TILE >> 4)), b = kd + (uint64_t)((gj & 1) * (P::TILE >> 4));
+        const uint64_t b = kd + (uint64_t)(st * (P::TILE >> 4)), qa = qd + (uint64_t)(s.two && g ? P::TILE >> 4 : 0);
 #pragma unroll
-          for (int ks = 0; ks < Dh / 16; ++ks) {
-            const uint64_t off = (uint64_t)((ks >> 2) * (P::SLAB >> 4) + (ks & 3) * 2);
-            mma_bf16(tmem + tile * 128, qa + off, b + off, id_s, ks > 0 ? 1u : 0u);
-          }
-          mma_commit(&sh.bars.s_full[tile]);
-          if (!s.two || tile == 1) mma_commit(&sh.bars.k_free[gj & 1]);
+        for (int ks = 0; ks < Dh / 16; ++ks) {
+          constexpr uint64_t step = P::SLAB >> 4;
+          const uint64_t off = (uint64_t)(ks >> 2) * step + (uint64_t)((ks & 3) * 2);
+          mma_bf16(g * 128, qa + off, b + off, id_s, ks > 0 ? 1u : 0u);
         }
-        __syncwarp();
+        mma_commit(&sh.bars.s_full[g]);
+        mma_commit(&sh.bars.k_free[g][st]);
       }
     }
     base += s.n;
-    ++segments;
-    at += s.n;
-    if (at < end) next_unit<MANY_QT, MANY_TOKENS>(a, u);
+    at = s.next;
+    if (at < end) next_unit<ManyShape>(a, u);
   }
 }
 
@@ -311,188 +401,301 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, int b, int i, int 
   return bits;
 }
 
-// The row's queries as fp16 in the operand's layout, times a power of two (see Queries in ts_attn.cu); returns the factor that
-// makes its scores exponents of two.  chunks c0 .. c1 - 1 (of eight channels) are written.
+// A warp's 32 rows of queries as fp16 in the operand's layout, times a power of two (see Queries in ts_attn.cu): Dh/8 lanes a
+// row and load (a row a lane would touch 32 lines with every load).  Returns the factor that makes the scores of the lane's
+// own row exponents of two.  chunks c0 .. c1 - 1 (of eight channels) are written.
 template <int Dh>
-__device__ __forceinline__ float load_query(const AttnArgs& a, const AttnUnit& u, int h, int idx, unsigned char* dst, int row, int c0, int c1) {
-  uint4 v[Dh / 8];
-  const bool used = idx < u.rows * a.d.G;
-  const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(a.q) + ((size_t)u.b * a.rcap + idx / a.d.G) * a.ldq + (size_t)(h * a.d.G + idx % a.d.G) * Dh;
-  uint32_t top = 0;   // largest magnitude, as bf16 bits in both halves (magnitudes compare as integers)
+__device__ __forceinline__ float load_queries(const AttnArgs& a, const AttnUnit& u, int h, int idx0, unsigned char* dst, int row0, int c0, int c1) {
+  constexpr int L = Dh / 8, R = 32 / L;   // lanes a row, rows a load
+  const int lane = threadIdx.x & 31, c = lane % L, sub = lane / L;
+  float mine = 0.f;
+#pragma unroll 1
+  for (int k0 = 0; k0 < 32 / R; k0 += 8) {   // (eight loads in flight; code that runs once a unit is fetched more slowly than it runs)
+    uint4 v[8];
 #pragma unroll
-  for (int c = 0; c < Dh / 8; ++c) {
-    v[c] = used ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0u, 0u, 0u, 0u);
-    top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[c].x & 0x7FFF7FFFu, v[c].y & 0x7FFF7FFFu), __vmaxu2(v[c].z & 0x7FFF7FFFu, v[c].w & 0x7FFF7FFFu)));
+    for (int k = 0; k < 8; ++k) {
+      const int idx = idx0 + (k0 + k) * R + sub;
+      const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(a.q) + head_row(a, u.b, h, idx, a.ldq);
+      v[k] = idx < u.rows * a.d.G ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      // largest magnitude, as bf16 bits (magnitudes compare as integers)
+      uint32_t top = __vmaxu2(__vmaxu2(v[k].x & 0x7FFF7FFFu, v[k].y & 0x7FFF7FFFu), __vmaxu2(v[k].z & 0x7FFF7FFFu, v[k].w & 0x7FFF7FFFu));
+#pragma unroll
+      for (int x = L / 2; x; x >>= 1) top = __vmaxu2(top, __shfl_xor_sync(~0u, top, x));
+      const int e = max((int)(max(top & 0xFFFFu, top >> 16) >> 7), 20);
+      // (the sign of the scale goes to the queries: the largest score is the factor times the largest sum)
+      const float up = copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk);
+      const float f = __shfl_sync(~0u, fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23), lane % R * L);
+      if (lane / R == k0 + k) mine = f;
+      if (c < c0 || c >= c1) continue;
+      float x[8];
+      unpack_bf16x8(v[k], x);
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = as_u32(__floats2half2_rn(x[2 * i] * up, x[2 * i + 1] * up));
+      const int row = row0 + (k0 + k) * R + sub;
+      *reinterpret_cast<uint4*>(dst + (c >> 3) * ManyPlan<Dh>::SLAB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
-  const uint32_t big = max(top & 0xFFFFu, top >> 16);
-  const int e = max((int)(big >> 7), 20);
-  // (the sign of the scale goes to the queries: the largest score is the factor times the largest sum)
-  const float up = copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk);
+  return mine;
+}
+
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+  return r;
+}
+
+// n columns of the thread's row in tensor memory times r.  Not often.
+__device__ __forceinline__ void scale_columns(uint32_t at, int n, float r) {
+#pragma unroll 1
+  for (int c = 0; c < n; c += 16) {
+    uint32_t x[16];
+    tmem_ld16_issue(at + c, x);
+    tmem_ld16_wait(x);
 #pragma unroll
-  for (int c = 0; c < Dh / 8; ++c) {
-    if (c < c0 || c >= c1) continue;
-    float x[8];
-    unpack_bf16x8(v[c], x);
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = as_u32(__floats2half2_rn(x[2 * i] * up, x[2 * i + 1] * up));
-    *reinterpret_cast<uint4*>(dst + (c >> 3) * ManyPlan<Dh>::SLAB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * r);
+    tmem_st16(at + c, x);
   }
-  return fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23);
+  tmem_st_wait();
+}
+
+// What a softmax thread keeps of its row: weights are 2^(f s - ref), l their sum.  ref moves when a score passes it by ROOM +
+// LIFT: weights stay below 2^15, and LIFT keeps small ones out of fp16's subnormals.  References are whole numbers, so that
+// what was computed with the old one is taken to the new one without another rounding.
+struct SoftRow {
+  static constexpr float ROOM = 8.f, LIFT = 7.f;
+  float f, m, ref, l;
+  // the factor from the old reference to the new one
+  __device__ __forceinline__ float move(float top) {
+    float r = 1.f;
+    if (top > m) {
+      const float now = ceilf(top) - LIFT;
+      r = m == -INFINITY ? 0.f : ex2(ref - now);
+      ref = now; m = now + LIFT + ROOM; l *= r;
+    }
+    return r;
+  }
+};
+
+__device__ __forceinline__ float largest(const uint32_t (&x)[32]) {
+  float t[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) t[k] = fmaxf(__uint_as_float(x[k]), __uint_as_float(x[k + 4]));
+#pragma unroll
+  for (int k = 8; k < 32; k += 8)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = fmaxf(t[i], fmaxf(__uint_as_float(x[k + i]), __uint_as_float(x[k + i + 4])));
+  return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+}
+
+// scores of tokens that the row does not see (bits not set) become -inf
+__device__ __forceinline__ void mask_scores(uint32_t (&x)[32], uint32_t on) {
+#pragma unroll
+  for (int k = 0; k < 32; ++k) x[k] = on >> k & 1u ? x[k] : 0xFF800000u;
+}
+
+// 32 scores to fp16 weights: two a fused multiply-add and an addition (f32x2).
+__device__ __forceinline__ void weigh(const uint32_t (&x)[32], SoftRow& row, uint32_t (&w)[16]) {
+  const uint64_t f2 = pair(row.f, row.f), r2 = pair(-row.ref, -row.ref);
+  uint64_t l2[2] = {pair(row.l, 0.f), pair(0.f, 0.f)};
+#pragma unroll
+  for (int k = 0; k < 32; k += 2) {
+    float e0, e1;
+    unpair(fma2(pair(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, r2), e0, e1);
+    e0 = ex2(e0); e1 = ex2(e1);
+    l2[k / 2 & 1] = add2(l2[k / 2 & 1], pair(e0, e1));
+    w[k / 2] = as_u32(__floats2half2_rn(e0, e1));
+  }
+  float l0, l1;
+  unpair(add2(l2[0], l2[1]), l0, l1);
+  row.l = l0 + l1;
 }
 
 template <int Dh>
-__device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* smem, AttnUnit u, long long start, long long end) {
+__device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* smem) {
   using P = ManyPlan<Dh>;
-  constexpr float ROOM = 8.f, LIFT = 7.f;
+  const ManyPiece piece = my_piece(sh);
+  AttnUnit u = piece.u;
+  const long long end = piece.end;
   volatile int* abort = (volatile int*)&sh.abort;
-  const int grp = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31;
-  const uint32_t lanes = (uint32_t)(row & 96) << 16, ts = sh.tmem + lanes + grp * 128, to = sh.tmem + lanes + P::O;
+  // group, half of a step's tokens, row of the tile (a warp reaches the 32 rows of its number modulo 4)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = warp >> 3, hh = (warp >> 2) & 1, quad = warp & 3, row = quad * 32 + lane;
+  const uint32_t lanes = (uint32_t)(quad * 32) << 16, ts = lanes + grp * 128 + hh * 64, to = lanes + P::O;
+  // the warp's own part of the group's query tile, which results leave through
+  unsigned char* stage = smem + P::Q + grp * P::TILE + (Dh == 128 ? hh * P::SLAB + quad * 4096 : quad * 4096 + hh * 2048);
   uint32_t count = 0;   // products of this group
   int base = 0;
-  bool alive = true;
-  for (long long at = start; at < end;) {
-    const ManySegment s = many_segment<Dh>(a, u, start, end, at);
-    const int idx = s.first + (s.two ? grp * 128 : 0) + row, i = idx / a.d.G;
-    // both groups write half of a shared tile; their own where they have one
-    const float f = load_query<Dh>(a, u, s.h, idx, smem + P::Q + (s.two ? grp * P::TILE : 0), row, s.two ? 0 : grp * (Dh / 16), s.two ? Dh / 8 : (grp + 1) * (Dh / 16));
+  bool alive = true, apart = false;   // apart: the groups had tiles of their own in the unit before
+  for (long long at = piece.start; at < end;) {
+    const ManySegment s = many_segment(a, u, at, end);
+    const int idx = s.first + (s.two ? grp * 128 : 0) + row, i = tree_row(a, idx);
+    // a shared tile is written by all, and the first group's products of the unit before may still read it; their own where
+    // they have one (the part of it that the warp's own results have left through)
+    if (!s.two && apart) soft_sync();
+    apart = s.two;
+    SoftRow my{0.f, -INFINITY, 0.f, 0.f};
+    {
+      const int n = s.two ? Dh / 16 : Dh / 32, c0 = n * (s.two ? hh : grp * 2 + hh);
+      // (a scale of 0: a factor that makes every finite score 0 and leaves a masked one, -inf, at weight 0)
+      my.f = fmaxf(1e-30f, load_queries<Dh>(a, u, s.h, idx - lane, smem + P::Q + (s.two ? grp * P::TILE : 0), row - lane, c0, c0 + n));
+    }
     fence_async_smem();
     __syncwarp();
-    if (lane == 0) mbar_arrive(&sh.bars.q_full);
-    float m = -INFINITY, ref = 0.f, l = 0.f;
+    if (lane == 0) {   // (sixteen arrivals: of all warps, or twice of the group's own)
+      mbar_arrive(&sh.bars.q_full[grp]);
+      mbar_arrive(&sh.bars.q_full[s.two ? grp : grp ^ 1]);
+    }
     int done = 0;   // products of this segment
-    for (int j = s.two ? 0 : grp; j < s.n && alive; j += s.two ? 1 : 2) {
-      alive = __all_sync(~0u, mbar_wait(&sh.bars.s_full[grp], count & 1u, abort, nullptr, a.limit));
-      if (!alive) break;
+    // (no way out of the loop: the two warps of 32 rows meet in it, whether or not a wait has given up)
+#pragma unroll 1
+    for (int j = s.two ? 0 : grp; j < s.n; j += s.two ? 1 : 2) {
+      if (alive) alive = __all_sync(~0u, mbar_wait(&sh.bars.s_full[grp], count & 1u, abort, nullptr, a.limit));
       tc_fence_after();
       const int tok0 = (s.j0 + j) * MANY_TOKENS;
-      const unsigned here = sh.present[(base + j) % MANY_PRESENT];
-      const bool masked = tok0 > u.seq - MANY_TOKENS || here != 0xFFu;
-      auto seen = [&](int c) {   // tokens of chunk c that the row sees
-        const unsigned two = here >> (2 * c);
-        return ((two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u)) & sees32(a, u.b, i, tok0 + 32 * c - u.seq, u.rows);
-      };
+      const unsigned here = sh.present[(base + j) % MANY_PRESENT] >> (4 * hh) & 0xFu;
+      uint32_t on[2] = {~0u, ~0u}, x[32];
+      if (tok0 > u.seq - MANY_TOKENS || here != 0xFu) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          on[c] = ((here >> (2 * c) & 1u ? 0xFFFFu : 0u) | (here >> (2 * c + 1) & 1u ? 0xFFFF0000u : 0u)) & sees32(a, u.b, i, tok0 + 64 * hh + 32 * c - u.seq, u.rows);
+      }
       float top = -INFINITY;
+      if (alive) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t r[32];
-        tmem_ld32(ts + 32 * c, r);
-        tmem_ld_wait();
-        if (masked) {
-          const uint32_t on = seen(c);
-#pragma unroll
-          for (int k = 0; k < 32; ++k) r[k] = on >> k & 1u ? r[k] : 0xFF800000u;
+        for (int c = 0; c < 2; ++c) {
+          tmem_ld32(ts + 32 * c, x);
+          tmem_ld32_wait(x);
+          if (__any_sync(~0u, on[c] != ~0u)) mask_scores(x, on[c]);
+          top = fmaxf(top, largest(x));
         }
-#pragma unroll
-        for (int k = 0; k < 32; k += 2) top = fmaxf(top, fmaxf(__uint_as_float(r[k]), __uint_as_float(r[k + 1])));
       }
-      top = top == -INFINITY ? top : top * f;
-      if (__any_sync(~0u, top > m)) {
-        // (weights of at most 2^15; the reference moves when a score passes it by more than ROOM)
-        const bool up = top > m;
-        const float r = m == -INFINITY ? 0.f : ex2(ref - (top - LIFT));
-        if (up) { ref = top - LIFT; l *= r; }
-        if (__any_sync(~0u, up && m != -INFINITY)) {
-          // the products before have to be in the sum that is scaled
+      sh.top[grp][hh][row] = top;
+      pair_sync(grp * 4 + quad);
+      top = fmaxf(top, sh.top[grp][hh ^ 1][row]) * my.f;
+      if (alive && __any_sync(~0u, top > my.m)) {
+        const float r = my.move(top);
+        if (done > 0) {   // the products before have to be in the sum that is scaled
           alive = __all_sync(~0u, mbar_wait(&sh.bars.o_full[grp], (count - 1u) & 1u, abort, nullptr, a.limit));
-          if (!alive) break;
           tc_fence_after();
-          const float k = up ? r : 1.f;
-#pragma unroll
-          for (int c = 0; c < Dh / 32; ++c) {
-            uint32_t x[32];
-            tmem_ld32(to + grp * Dh + 32 * c, x);
-            tmem_ld_wait();
-#pragma unroll
-            for (int q = 0; q < 32; ++q) x[q] = __float_as_uint(__uint_as_float(x[q]) * k);
-            tmem_st32(to + grp * Dh + 32 * c, x);
-          }
-          tmem_st_wait();
+          scale_columns(to + grp * Dh + hh * (Dh / 2), Dh / 2, r);
         }
-        if (up) m = top + ROOM;
       }
-      float l0 = 0.f, l1 = 0.f;
+      if (alive) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t r[32], w[16];
-        tmem_ld32(ts + 32 * c, r);
-        tmem_ld_wait();
-        const uint32_t on = masked ? seen(c) : ~0u;
-#pragma unroll
-        for (int k = 0; k < 32; k += 2) {
-          float e0 = ex2(fmaf(__uint_as_float(r[k]), f, -ref)), e1 = ex2(fmaf(__uint_as_float(r[k + 1]), f, -ref));
-          if (masked) { e0 = on >> k & 1u ? e0 : 0.f; e1 = on >> (k + 1) & 1u ? e1 : 0.f; }
-          l0 += e0; l1 += e1;
-          w[k / 2] = as_u32(__floats2half2_rn(e0, e1));
+        for (int c = 0; c < 2; ++c) {
+          uint32_t w[16];
+          tmem_ld32(ts + 32 * c, x);
+          tmem_ld32_wait(x);
+          if (__any_sync(~0u, on[c] != ~0u)) mask_scores(x, on[c]);
+          weigh(x, my, w);
+          tmem_st16(ts + 16 * c, w);   // (the weights replace scores that are taken)
         }
-        tmem_st16(ts + 16 * c, w);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.bars.p_full[grp]);
       }
-      l += l0 + l1;
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.bars.p_full[grp]);
       ++count;
       ++done;
     }
-    // ---- results: a group's own tile, or half of the channels of the rows that both share
+    // ---- results: by group and half, channels of the group's own tile or of the rows that the groups share
     if (alive && done > 0) alive = __all_sync(~0u, mbar_wait(&sh.bars.o_full[grp], (count - 1u) & 1u, abort, nullptr, a.limit));
-    float sum = l, top = m == -INFINITY ? m : ref, w0 = 1.f, w1 = 0.f;   // weights of the groups' parts
-    bool other = false;
-    if (!s.two) {
-      sh.ml[grp][row][0] = top; sh.ml[grp][row][1] = l;
-      soft_sync();            // (both groups' products are complete: each has waited for its own)
-      const float t0 = sh.ml[0][row][0], t1 = sh.ml[1][row][0], l0 = sh.ml[0][row][1], l1 = sh.ml[1][row][1];
+    sh.ml[grp][hh][row][0] = my.m == -INFINITY ? -INFINITY : my.ref;
+    sh.ml[grp][hh][row][1] = my.l;
+    if (s.two) pair_sync(grp * 4 + quad);
+    else soft_sync();         // (both groups' products are complete: each has waited for its own)
+    float sum, top, w0 = 1.f, w1 = 0.f;   // weights of the groups' parts
+    if (s.two) {
+      top = sh.ml[grp][0][row][0];
+      sum = sh.ml[grp][0][row][1] + sh.ml[grp][1][row][1];
+    } else {
+      const float t0 = sh.ml[0][0][row][0], t1 = sh.ml[1][0][row][0];
       top = fmaxf(t0, t1);
       w0 = part_weight(t0, top); w1 = part_weight(t1, top);
-      sum = w0 * l0 + w1 * l1;
-      other = s.n > 1;        // else the second group's sum was never written
+      sum = w0 * (sh.ml[0][0][row][1] + sh.ml[0][1][row][1]) + w1 * (sh.ml[1][0][row][1] + sh.ml[1][1][row][1]);
     }
+    const bool other = !s.two && s.n > 1;   // (with one step the second group's sum was never written)
     if (!alive || *abort) sum = NAN;
     tc_fence_after();
-    const bool used = idx < u.rows * a.d.G;
-    const size_t piece = ((size_t)blockIdx.x * 2 + (start > u.t0 ? 0 : 1)) * MANY_QT + (s.two ? grp * 128 : 0) + row;
+    const int rows = u.rows * a.d.G;
+    const size_t slot = ((size_t)blockIdx.x * 2 + (piece.start > u.t0 ? 0 : 1)) * MANY_QT + (s.two ? grp * 128 : 0) + row;
     const float inv = s.whole ? row_inv(sum) * a.vo : 1.f;
-    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(a.out) + (used ? out_row(a, u.b, s.h, idx) : 0);
-    const int c_lo = s.two ? 0 : grp * (Dh / 64), c_hi = s.two ? Dh / 32 : (grp + 1) * (Dh / 64);
+    const int n = s.two ? Dh / 64 : 1, c_lo = (s.two ? hh : grp * 2 + hh) * n, c_hi = min(c_lo + n, Dh / 32);   // groups of 32 channels
+#pragma unroll 1
     for (int c = c_lo; c < c_hi; ++c) {
       uint32_t x[32];
       tmem_ld32(to + (s.two ? grp * Dh : 0) + 32 * c, x);
-      tmem_ld_wait();
-      float v[32];
+      tmem_ld32_wait(x);
 #pragma unroll
-      for (int k = 0; k < 32; ++k) v[k] = w0 * __uint_as_float(x[k]);
+      for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(w0 * __uint_as_float(x[k]) * inv);
       if (other) {
-        tmem_ld32(to + Dh + 32 * c, x);
-        tmem_ld_wait();
+        uint32_t y[16];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] += w1 * __uint_as_float(x[k]);
-      }
-      if (used && s.whole) {
+        for (int half = 0; half < 2; ++half) {
+          tmem_ld16_issue(to + Dh + 32 * c + 16 * half, y);
+          tmem_ld16_wait(y);
 #pragma unroll
-        for (int k = 0; k < 32; k += 8) {
-          uint32_t w[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const __nv_bfloat162 h2 = __floats2bfloat162_rn(v[k + 2 * q] * inv, v[k + 2 * q + 1] * inv);
-            w[q] = *reinterpret_cast<const uint32_t*>(&h2);
-          }
-          *reinterpret_cast<uint4*>(out + 32 * c + k) = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int k = 0; k < 16; ++k) x[16 * half + k] = __float_as_uint(fmaf(w1 * inv, __uint_as_float(y[k]), __uint_as_float(x[16 * half + k])));
         }
-      } else if (used) {
+      }
+      // through the stage in pieces of 16 bytes, so that rows leave in whole lines: bf16 in one round, fp32 in one or two
+      constexpr int ROOM = Dh / 16;   // pieces of a staged row
+      const int bits = s.whole || ROOM == 4 ? 2 : 3, rounds = s.whole ? 1 : 8 >> bits;
+#pragma unroll 1
+      for (int rd = 0; rd < rounds; ++rd) {
+        auto put = [&](int k, uint4 v) { *reinterpret_cast<uint4*>(stage + lane * Dh + ((k ^ (lane & (ROOM - 1))) << 4)) = v; };
+        if (s.whole) {
 #pragma unroll
-        for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(a.part + piece * Dh + 32 * c + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+          for (int k = 0; k < 4; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(x[8 * k + 2 * q]), __uint_as_float(x[8 * k + 2 * q + 1]));
+              w[q] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+            put(k, make_uint4(w[0], w[1], w[2], w[3]));
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (ROOM == 8 || k / 4 == rd) put(k & (ROOM - 1), make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]));
+        }
+        __syncwarp();
+        for (int e = lane; e < 32 << bits; e += 32) {
+          const int r = e >> bits, k = e - (r << bits), id = idx - lane + r;
+          if (id >= rows) break;   // (rows rise with e)
+          const uint4 t = *reinterpret_cast<const uint4*>(stage + r * Dh + ((k ^ (r & (ROOM - 1))) << 4));
+          if (s.whole) reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row(a, u.b, s.h, id) + 32 * c)[k] = t;
+          else reinterpret_cast<uint4*>(a.part + (slot - lane + r) * Dh + 32 * c)[rd * 4 + k] = t;
+        }
+        __syncwarp();
       }
     }
-    if (used && (s.two || grp == 0)) {
-      if (!s.whole) { a.part_ml[2 * piece] = top; a.part_ml[2 * piece + 1] = sum; }
+    if (idx < rows && hh == 0 && (s.two || grp == 0)) {
+      if (!s.whole) { a.part_ml[2 * slot] = top; a.part_ml[2 * slot + 1] = sum; }
       else if (a.lse) a.lse[lse_row(a, u.b, s.h, idx)] = row_lse(top, sum);
     }
     tc_fence_before();
-    if (!s.two) soft_sync();   // both have read both sums, before the next unit's products overwrite them
+    // all have read the sums and left the stages, before the next unit's products and queries overwrite them
+    if (s.two) pair_sync(grp * 4 + quad);
+    else soft_sync();
     base += s.n;
-    at += s.n;
-    if (at < end) next_unit<MANY_QT, MANY_TOKENS>(a, u);
+    at = s.next;
+    if (at < end) next_unit<ManyShape>(a, u);
   }
 }
 
@@ -508,30 +711,36 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
     sh.abort = 0;
     for (int s = 0; s < MANY_RAW; ++s) { mbar_init(&b.raw_full[s], 1); mbar_init(&b.raw_free[s], MANY_CONV); }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(&b.k_full[s], MANY_CONV); mbar_init(&b.k_free[s], 1);
-      mbar_init(&b.v_full[s], MANY_CONV); mbar_init(&b.v_free[s], 1);
-      mbar_init(&b.s_full[s], 1); mbar_init(&b.p_full[s], 4); mbar_init(&b.o_full[s], 1);
+      mbar_init(&b.k_full[s], MANY_CONV / 2); mbar_init(&b.k_free[0][s], 1); mbar_init(&b.k_free[1][s], 1);
+      mbar_init(&b.v_full[s], MANY_CONV / 2); mbar_init(&b.v_free[0][s], 1); mbar_init(&b.v_free[1][s], 1);
+      mbar_init(&b.q_full[s], MANY_SOFT); mbar_init(&b.s_full[s], 1); mbar_init(&b.p_full[s], MANY_SOFT / 2); mbar_init(&b.o_full[s], 1);
     }
-    mbar_init(&b.q_full, MANY_SOFT);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_wait();
   pdl_launch_dependents();
   AttnUnit u;
   long long start, end;
-  int active;
-  if (!attn_locate<MANY_QT, MANY_TOKENS, MANY_THREADS>(a, u, start, end, active)) return;
+  if (!attn_locate<ManyShape, MANY_THREADS>(a, u, start, end)) return;
   if (warp == MANY_ISSUE) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (threadIdx.x == 0) { sh.piece.u = u; sh.piece.start = start; sh.piece.end = end; }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp < MANY_SOFT) many_softmax<Dh>(a, sh, smem, u, start, end);
-  else if (warp < MANY_ISSUE) many_convert<Dh>(a, sh, smem, (int)(end - start));
-  else if (warp == MANY_ISSUE) many_issue<Dh>(a, sh, smem, u, start, end);
-  else many_load<Dh>(a, sh, smem + P::R, u, start, end);
+  if (sh.tmem != 0u) sh.abort = 1;   // (cannot be: 512 columns were asked for)
+  if (warp < MANY_SOFT) {
+    many_softmax<Dh>(a, sh, smem);
+  } else {
+    if (warp < MANY_SOFT + MANY_CONV / 2)
+      many_convert<KeyPart<Dh>, Dh>(a, sh, smem + P::R, smem + P::K, sh.bars.k_full, sh.bars.k_free, threadIdx.x - MANY_SOFT * 32);
+    else if (warp < MANY_ISSUE)
+      many_convert<ValuePart<Dh>, Dh>(a, sh, smem + P::R, smem + P::V, sh.bars.v_full, sh.bars.v_free, threadIdx.x - MANY_SOFT * 32 - MANY_CT);
+    else if (warp == MANY_ISSUE) { if (elect_one()) many_issue<Dh>(a, sh, smem); }
+    else if (warp == MANY_LOAD) many_load<Dh>(a, sh, smem + P::R);
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
