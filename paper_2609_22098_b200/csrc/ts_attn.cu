@@ -402,76 +402,72 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 }
 
 // ------------------------------------------------------------------------------------------------
-// Join: RW warps a (cut unit, query row).  The pieces are added in their order, so results do not depend on timing.
+// Join: a CTA takes up to 32 rows of a cut unit, a warp a row; where there are many pieces, all its warps one row after the
+// other.  The pieces are added in an order that depends on their number only.
 // ------------------------------------------------------------------------------------------------
-constexpr int JOIN_WARPS = 8;
+constexpr int JOIN_WARPS = 8, JOIN_ROWS = 32;
 
-template <int Dh, int RW, typename T>
+template <int Dh, typename T>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnArgs a, int QT) {
-  constexpr int V = Dh / 32, ROWS = JOIN_WARPS / RW;
+  constexpr int V = Dh / 32;
   __shared__ float acc[JOIN_WARPS][Dh], red[JOIN_WARPS][2];
   pdl_wait();
   pdl_launch_dependents();
   const AttnRecord r = a.records[blockIdx.x];
   if (r.first < 0) return;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, part = w % RW, w0 = w - part;
-  const int h = r.v / r.nq, row = blockIdx.y * ROWS + w / RW, idx = (r.v - h * r.nq) * QT + row, n = r.last - r.first + 1;
-  const bool used = idx < request_rows(a.n_nodes, r.b, a.rcap) * a.d.G;
-  // piece k: the first begins at or before the unit and is its CTA's last; the others begin within it
-  auto at = [&](int k) { return ((size_t)(r.first + k) * 2 + (k == 0 ? 1 : 0)) * QT + row; };
-  float top = -INFINITY;
-  if (used)
-    for (int k = part * 32 + lane; k < n; k += RW * 32) top = fmaxf(top, a.part_ml[2 * at(k)]);
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = r.last - r.first + 1;
+  const int h = r.v / r.nq, first = (r.v - h * r.nq) * QT, r0 = blockIdx.y * JOIN_ROWS;
+  const int rows = min(min(QT, r0 + JOIN_ROWS), request_rows(a.n_nodes, r.b, a.rcap) * a.d.G - first);   // of the tile, that are there
+  const int rw = n > 2 * JOIN_WARPS ? JOIN_WARPS : 1, part = rw > 1 ? w : 0;                             // warps a row
+  for (int row = r0 + (rw > 1 ? 0 : w); row < rows; row += rw > 1 ? 1 : JOIN_WARPS) {
+    // piece k: the first begins at or before the unit and is its CTA's last; the others begin within it
+    auto at = [&](int k) { return ((size_t)(r.first + k) * 2 + (k == 0 ? 1 : 0)) * QT + row; };
+    float top = -INFINITY;
+    for (int k = lane; k < n; k += 32) top = fmaxf(top, a.part_ml[2 * at(k)]);
 #pragma unroll
-  for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
-  if (RW > 1) {
-    if (lane == 0) red[w][0] = top;
-    __syncthreads();
+    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
+    float sum = 0.f, x[V];
 #pragma unroll
-    for (int k = 0; k < RW; ++k) top = fmaxf(top, red[w0 + k][0]);
-  }
-  float sum = 0.f, x[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = 0.f;
-  if (used) {
+    for (int i = 0; i < V; ++i) x[i] = 0.f;
 #pragma unroll 4
-    for (int k = part; k < n; k += RW) {
-      const float wgt = part_weight(a.part_ml[2 * at(k)], top);
-      sum += wgt * a.part_ml[2 * at(k) + 1];
+    for (int k = part; k < n; k += rw) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * at(k));
+      const float wgt = part_weight(ml.x, top);
+      sum += wgt * ml.y;
 #pragma unroll
       for (int i = 0; i < V; ++i) x[i] += wgt * a.part[at(k) * Dh + lane + 32 * i];
     }
-  }
-  if (RW > 1) {
+    if (rw > 1) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[w][lane + 32 * i] = x[i];
-    if (lane == 0) red[w][1] = sum;
-    __syncthreads();
-    if (part > 0 || !used) return;
+      for (int i = 0; i < V; ++i) acc[w][lane + 32 * i] = x[i];
+      if (lane == 0) red[w][1] = sum;
+      __syncthreads();
+      sum = 0.f;
 #pragma unroll
-    for (int k = 1; k < RW; ++k) {
-      sum += red[w0 + k][1];
+      for (int i = 0; i < V; ++i) x[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] += acc[w0 + k][lane + 32 * i];
+      for (int k = 0; k < JOIN_WARPS; ++k) {
+        sum += red[k][1];
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] += acc[k][lane + 32 * i];
+      }
+      __syncthreads();
+      if (w > 0) continue;
     }
-  }
-  if (!used) return;
-  T* out = reinterpret_cast<T*>(a.out) + out_row(a, r.b, h, idx);
-  const float inv = row_inv(sum) * a.vo;
+    const int idx = first + row;
+    T* out = reinterpret_cast<T*>(a.out) + out_row(a, r.b, h, idx);
+    const float inv = row_inv(sum) * a.vo;
 #pragma unroll
-  for (int i = 0; i < V; ++i) store_out(out + lane + 32 * i, x[i] * inv);
-  if (lane == 0 && a.lse) a.lse[lse_row(a, r.b, h, idx)] = row_lse(top, sum);
+    for (int i = 0; i < V; ++i) store_out(out + lane + 32 * i, x[i] * inv);
+    if (lane == 0 && a.lse) a.lse[lse_row(a, r.b, h, idx)] = row_lse(top, sum);
+  }
 }
 
-// Few rows are cut into more pieces: four warps a row there, two where tiles are large.
 cudaError_t attn_join(ts_ctx* ctx, const AttnArgs& a, int QT, bool f32, cudaStream_t st) {
   ProfScope ps(ctx, K_ATTN_JOIN, st);
-  const int rw = QT > 16 ? 2 : 4;
-  void (*kernel)(const AttnArgs, int);
-  if (rw == 2) kernel = a.d.Dh == 128 ? attn_join_kernel<128, 2, __nv_bfloat16> : attn_join_kernel<64, 2, __nv_bfloat16>;
-  else if (f32) kernel = a.d.Dh == 128 ? attn_join_kernel<128, 4, float> : attn_join_kernel<64, 4, float>;
-  else kernel = a.d.Dh == 128 ? attn_join_kernel<128, 4, __nv_bfloat16> : attn_join_kernel<64, 4, __nv_bfloat16>;
-  return launch_kernel(kernel, dim3(a.grid, QT * rw / JOIN_WARPS), dim3(JOIN_WARPS * 32), 0, st, true, a, QT);
+  void (*kernel)(const AttnArgs, int) = f32 ? (a.d.Dh == 128 ? attn_join_kernel<128, float> : attn_join_kernel<64, float>)
+                                            : (a.d.Dh == 128 ? attn_join_kernel<128, __nv_bfloat16> : attn_join_kernel<64, __nv_bfloat16>);
+  return launch_kernel(kernel, dim3(a.grid, (QT + JOIN_ROWS - 1) / JOIN_ROWS), dim3(JOIN_WARPS * 32), 0, st, true, a, QT);
 }
 
 static size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -516,6 +512,9 @@ cudaError_t attn_setup(ts_ctx* ctx) {
   allow(attn_few_kernel<128, 1, false>); allow(attn_few_kernel<128, 2, false>); allow(attn_few_kernel<128, 1, true>);
   allow(attn_few_kernel<64, 1, false>); allow(attn_few_kernel<64, 2, false>); allow(attn_few_kernel<64, 1, true>);
   if (e == cudaSuccess) e = attn_many_setup(ctx);
+  // the same split of L1 and shared memory as the kernels before it and after: an SM that changes it has to run empty first
+  auto shared = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); };
+  shared(attn_join_kernel<128, float>); shared(attn_join_kernel<64, float>); shared(attn_join_kernel<128, __nv_bfloat16>); shared(attn_join_kernel<64, __nv_bfloat16>);
   return e;
 }
 

@@ -57,11 +57,14 @@ __device__ __forceinline__ long long unit_set(const AttnArgs& a, int b, AttnUnit
 template <class S>
 __device__ __forceinline__ int unit_weight(const AttnUnit& u) { return S::WIDE == S::HALF ? S::WIDE : (u.v + 1) % u.nq == 0 ? u.wl : S::WIDE; }
 
+// (a division of 64 bits is a call of a hundred instructions; almost all of these fit 32)
+__device__ __forceinline__ long long divide(long long x, long long y) { return (unsigned long long)(x | y) >> 32 ? x / y : (long long)((unsigned)x / (unsigned)y); }
+
 // CTAs that take part, where piece c begins, and the piece in which place x lies
 template <class S>
-__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, total / (a.min_steps * S::WIDE))); }
-__device__ __forceinline__ long long piece_start(long long total, int active, int c) { return total * c / active; }
-__device__ __forceinline__ int piece_of(long long total, int active, long long x) { return (int)(((x + 1) * active + total - 1) / total) - 1; }
+__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, divide(total, a.min_steps * S::WIDE))); }
+__device__ __forceinline__ long long piece_start(long long total, int active, int c) { return divide(total * c, active); }
+__device__ __forceinline__ int piece_of(long long total, int active, long long x) { return (int)divide((x + 1) * active + total - 1, total) - 1; }
 
 template <class S>
 __device__ __forceinline__ void next_unit(const AttnArgs& a, AttnUnit& u) {
@@ -108,7 +111,7 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, lo
     for (int b = b0;; ++b) {
       const long long w = unit_set<S>(a, b, n);
       if (x0 < at + w) {
-        const long long head = w / a.d.Hkv, x = x0 - at, h = x / head, q = min((x - h * head) / ((long long)n.n * S::WIDE), (long long)n.nq - 1);
+        const long long head = divide(w, a.d.Hkv), x = x0 - at, h = divide(x, head), q = min(divide(x - h * head, (long long)n.n * S::WIDE), (long long)n.nq - 1);
         n.v = (int)(h * n.nq + q);
         n.t0 = at + h * head + q * n.n * S::WIDE;
         n.wt = unit_weight<S>(n);
@@ -119,7 +122,7 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, lo
     }
   __syncthreads();
   u = found;
-  long long j = (x0 - u.t0 + u.wt - 1) / u.wt;
+  long long j = divide(x0 - u.t0 + u.wt - 1, u.wt);
   if (j >= u.n && u.t0 + (long long)u.n * u.wt < total) { next_unit<S>(a, u); j = 0; }
   start = u.t0 + j * u.wt;
   const bool any = j < u.n && start < end;

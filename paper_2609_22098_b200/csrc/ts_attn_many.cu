@@ -89,8 +89,9 @@ struct ManyShared {
   uint32_t tmem;
   int abort;
   unsigned char present[MANY_PRESENT];   // a bit for each block of a step
-  float top[2][2][128];                  // largest scores of a step, by group and half
-  float ml[2][2][128][2];                // reference and sum of a row, by group and half
+  float f[2][128];                       // factors of the rows' scores, by tile
+  float top[2][2][128];                  // by group and half: largest scores of a step; at a unit's end the rows' references
+  float sum[2][2][128];                  // and sums
 };
 
 // Every role reads its own copy of the piece: kept in registers across the parting of the roles it was spilled in all of them.
@@ -401,25 +402,24 @@ __device__ __forceinline__ uint32_t sees32(const AttnArgs& a, int b, int i, int 
   return bits;
 }
 
-// A warp's 32 rows of queries as fp16 in the operand's layout, times a power of two (see Queries in ts_attn.cu): Dh/8 lanes a
-// row and load (a row a lane would touch 32 lines with every load).  Returns the factor that makes the scores of the lane's
-// own row exponents of two.  chunks c0 .. c1 - 1 (of eight channels) are written.
+// `count` (a multiple of eight) of a warp's 32 rows of queries, from row `from` on, as fp16 in the operand's layout, times a power of
+// two (see Queries in ts_attn.cu): Dh/8 lanes a row and load (a row a lane would touch 32 lines with every load).  f[row]: the
+// factor that makes the row's scores exponents of two.  The lane's own row: idx of the unit, `row` of the tile.
 template <int Dh>
-__device__ __forceinline__ float load_queries(const AttnArgs& a, const AttnUnit& u, int h, int idx0, unsigned char* dst, int row0, int c0, int c1) {
+__device__ __forceinline__ void load_queries(const AttnArgs& a, const AttnUnit& u, int h, int idx, int from, int count, unsigned char* dst, int row, float* f) {
   constexpr int L = Dh / 8, R = 32 / L;   // lanes a row, rows a load
   const int lane = threadIdx.x & 31, c = lane % L, sub = lane / L;
-  float mine = 0.f;
+  const long long own = idx < u.rows * a.d.G ? (long long)head_row(a, u.b, h, idx, a.ldq) : -1;
 #pragma unroll 1
-  for (int k0 = 0; k0 < 32 / R; k0 += 8) {   // (eight loads in flight; code that runs once a unit is fetched more slowly than it runs)
-    uint4 v[8];
+  for (int k0 = from; k0 < from + count; k0 += 8) {
+    uint4 v[8 / R];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int idx = idx0 + (k0 + k) * R + sub;
-      const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(a.q) + head_row(a, u.b, h, idx, a.ldq);
-      v[k] = idx < u.rows * a.d.G ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0u, 0u, 0u, 0u);
+    for (int k = 0; k < 8 / R; ++k) {
+      const long long at = __shfl_sync(~0u, own, k0 + k * R + sub);
+      v[k] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(a.q) + at) + c) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 8 / R; ++k) {
       // largest magnitude, as bf16 bits (magnitudes compare as integers)
       uint32_t top = __vmaxu2(__vmaxu2(v[k].x & 0x7FFF7FFFu, v[k].y & 0x7FFF7FFFu), __vmaxu2(v[k].z & 0x7FFF7FFFu, v[k].w & 0x7FFF7FFFu));
 #pragma unroll
@@ -427,19 +427,16 @@ __device__ __forceinline__ float load_queries(const AttnArgs& a, const AttnUnit&
       const int e = max((int)(max(top & 0xFFFFu, top >> 16) >> 7), 20);
       // (the sign of the scale goes to the queries: the largest score is the factor times the largest sum)
       const float up = copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk);
-      const float f = __shfl_sync(~0u, fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23), lane % R * L);
-      if (lane / R == k0 + k) mine = f;
-      if (c < c0 || c >= c1) continue;
+      const int r = row - lane + k0 + k * R + sub;
+      if (c == 0) f[r] = fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23);
       float x[8];
       unpack_bf16x8(v[k], x);
       uint32_t w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = as_u32(__floats2half2_rn(x[2 * i] * up, x[2 * i + 1] * up));
-      const int row = row0 + (k0 + k) * R + sub;
-      *reinterpret_cast<uint4*>(dst + (c >> 3) * ManyPlan<Dh>::SLAB + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(dst + (c >> 3) * ManyPlan<Dh>::SLAB + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
-  return mine;
 }
 
 __device__ __forceinline__ uint64_t pair(float x, float y) {
@@ -543,22 +540,21 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
   for (long long at = piece.start; at < end;) {
     const ManySegment s = many_segment(a, u, at, end);
     const int idx = s.first + (s.two ? grp * 128 : 0) + row, i = tree_row(a, idx);
-    // a shared tile is written by all, and the first group's products of the unit before may still read it; their own where
-    // they have one (the part of it that the warp's own results have left through)
+    // The warps of 32 rows load a share each, of their own tile or of the shared one, which the first group's products of the
+    // unit before may still read.
     if (!s.two && apart) soft_sync();
     apart = s.two;
-    SoftRow my{0.f, -INFINITY, 0.f, 0.f};
-    {
-      const int n = s.two ? Dh / 16 : Dh / 32, c0 = n * (s.two ? hh : grp * 2 + hh);
-      // (a scale of 0: a factor that makes every finite score 0 and leaves a masked one, -inf, at weight 0)
-      my.f = fmaxf(1e-30f, load_queries<Dh>(a, u, s.h, idx - lane, smem + P::Q + (s.two ? grp * P::TILE : 0), row - lane, c0, c0 + n));
-    }
+    load_queries<Dh>(a, u, s.h, idx, s.two ? 16 * hh : 16 * grp + 8 * hh, s.two ? 16 : 8, smem + P::Q + (s.two ? grp * P::TILE : 0), row, sh.f[s.two ? grp : 0]);
     fence_async_smem();
     __syncwarp();
     if (lane == 0) {   // (sixteen arrivals: of all warps, or twice of the group's own)
       mbar_arrive(&sh.bars.q_full[grp]);
       mbar_arrive(&sh.bars.q_full[s.two ? grp : grp ^ 1]);
     }
+    if (s.two) pair_sync(grp * 4 + quad);
+    else soft_sync();
+    // (a scale of 0: a factor that makes every finite score 0 and leaves a masked one, -inf, at weight 0)
+    SoftRow my{fmaxf(1e-30f, sh.f[s.two ? grp : 0][row]), -INFINITY, 0.f, 0.f};
     int done = 0;   // products of this segment
     // (no way out of the loop: the two warps of 32 rows meet in it, whether or not a wait has given up)
 #pragma unroll 1
@@ -614,19 +610,19 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
     }
     // ---- results: by group and half, channels of the group's own tile or of the rows that the groups share
     if (alive && done > 0) alive = __all_sync(~0u, mbar_wait(&sh.bars.o_full[grp], (count - 1u) & 1u, abort, nullptr, a.limit));
-    sh.ml[grp][hh][row][0] = my.m == -INFINITY ? -INFINITY : my.ref;
-    sh.ml[grp][hh][row][1] = my.l;
+    sh.top[grp][hh][row] = my.m == -INFINITY ? -INFINITY : my.ref;
+    sh.sum[grp][hh][row] = my.l;
     if (s.two) pair_sync(grp * 4 + quad);
     else soft_sync();         // (both groups' products are complete: each has waited for its own)
     float sum, top, w0 = 1.f, w1 = 0.f;   // weights of the groups' parts
     if (s.two) {
-      top = sh.ml[grp][0][row][0];
-      sum = sh.ml[grp][0][row][1] + sh.ml[grp][1][row][1];
+      top = sh.top[grp][0][row];
+      sum = sh.sum[grp][0][row] + sh.sum[grp][1][row];
     } else {
-      const float t0 = sh.ml[0][0][row][0], t1 = sh.ml[1][0][row][0];
+      const float t0 = sh.top[0][0][row], t1 = sh.top[1][0][row];
       top = fmaxf(t0, t1);
       w0 = part_weight(t0, top); w1 = part_weight(t1, top);
-      sum = w0 * (sh.ml[0][0][row][1] + sh.ml[0][1][row][1]) + w1 * (sh.ml[1][0][row][1] + sh.ml[1][1][row][1]);
+      sum = w0 * (sh.sum[0][0][row] + sh.sum[0][1][row]) + w1 * (sh.sum[1][0][row] + sh.sum[1][1][row]);
     }
     const bool other = !s.two && s.n > 1;   // (with one step the second group's sum was never written)
     if (!alive || *abort) sum = NAN;
@@ -746,6 +742,8 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
   tc_fence_after();
   if (warp == MANY_ISSUE) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(512u) : "memory");
 }
+
+static_assert(sizeof(ManyShared) + ManyPlan<128>::SMEM + 128 <= 227 * 1024, "shared memory");
 
 cudaError_t attn_many_setup(ts_ctx* ctx) {
   const cudaError_t e = allow_all_smem(attn_many_kernel<128>, ctx->max_smem);
