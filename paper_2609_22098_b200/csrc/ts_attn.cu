@@ -402,13 +402,13 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 }
 
 // ------------------------------------------------------------------------------------------------
-// Join: a CTA takes up to 32 rows of a cut unit, a warp a row; where there are many pieces, all its warps one row after the
+// Join: a CTA takes some rows of a cut unit, a warp a row; where there are many pieces, all its warps one row after the
 // other.  The pieces are added in an order that depends on their number only.
 // ------------------------------------------------------------------------------------------------
-constexpr int JOIN_WARPS = 8, JOIN_ROWS = 32;
+constexpr int JOIN_WARPS = 8;
 
 template <int Dh, typename T>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnArgs a, int QT) {
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnArgs a, int QT, int per) {
   constexpr int V = Dh / 32;
   __shared__ float acc[JOIN_WARPS][Dh], red[JOIN_WARPS][2];
   pdl_wait();
@@ -416,8 +416,8 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnAr
   const AttnRecord r = a.records[blockIdx.x];
   if (r.first < 0) return;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = r.last - r.first + 1;
-  const int h = r.v / r.nq, first = (r.v - h * r.nq) * QT, r0 = blockIdx.y * JOIN_ROWS;
-  const int rows = min(min(QT, r0 + JOIN_ROWS), request_rows(a.n_nodes, r.b, a.rcap) * a.d.G - first);   // of the tile, that are there
+  const int h = r.v / r.nq, first = (r.v - h * r.nq) * QT, r0 = blockIdx.y * per;
+  const int rows = min(min(QT, r0 + per), request_rows(a.n_nodes, r.b, a.rcap) * a.d.G - first);   // of the tile, that are there
   const int rw = n > 2 * JOIN_WARPS ? JOIN_WARPS : 1, part = rw > 1 ? w : 0;                             // warps a row
   for (int row = r0 + (rw > 1 ? 0 : w); row < rows; row += rw > 1 ? 1 : JOIN_WARPS) {
     // piece k: the first begins at or before the unit and is its CTA's last; the others begin within it
@@ -465,9 +465,11 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnAr
 
 cudaError_t attn_join(ts_ctx* ctx, const AttnArgs& a, int QT, bool f32, cudaStream_t st) {
   ProfScope ps(ctx, K_ATTN_JOIN, st);
-  void (*kernel)(const AttnArgs, int) = f32 ? (a.d.Dh == 128 ? attn_join_kernel<128, float> : attn_join_kernel<64, float>)
+  // rows a CTA: few rows are cut into many pieces, which a CTA's warps share; many rows would be many CTAs
+  const int per = QT > 16 ? 32 : 2;
+  void (*kernel)(const AttnArgs, int, int) = f32 ? (a.d.Dh == 128 ? attn_join_kernel<128, float> : attn_join_kernel<64, float>)
                                             : (a.d.Dh == 128 ? attn_join_kernel<128, __nv_bfloat16> : attn_join_kernel<64, __nv_bfloat16>);
-  return launch_kernel(kernel, dim3(a.grid, (QT + JOIN_ROWS - 1) / JOIN_ROWS), dim3(JOIN_WARPS * 32), 0, st, true, a, QT);
+  return launch_kernel(kernel, dim3(a.grid, (QT + per - 1) / per), dim3(JOIN_WARPS * 32), 0, st, true, a, QT, per);
 }
 
 static size_t round256(size_t n) { return (n + 255) / 256 * 256; }

@@ -194,15 +194,19 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
 
 // ---- converters ---------------------------------------------------------------------------------------------------------
 // A thread's part of 64 raw tokens.  It is read at once, so that the ring's slot is free again before anything is converted.
-// K: Dh/8 bytes of the codes of two tokens, with their scales.
+// K: Dh/8 bytes of the codes of some tokens, with their scales.  A warp's lanes have eight tokens and the four quarters of a row,
+// shifted by a quarter every two tokens, so that neither the reads nor the writes of eight lanes meet in a bank.
 template <int Dh>
 struct KeyPart {
   static constexpr int W = Dh / 32, N = 256 / MANY_CT;
   uint32_t k[N][W], s[N];
+  static __device__ __forceinline__ int token(int tid, int n) { return n * (MANY_CT / 4) + (tid >> 5) * 8 + (tid & 7); }
+  static __device__ __forceinline__ int quarter(int tid) { return (((tid & 7) >> 1) + ((tid & 31) >> 3)) & 3; }
   __device__ __forceinline__ void read(const unsigned char* raw, int tid) {
+    const int q = quarter(tid);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int tok = (tid >> 2) + n * (MANY_CT / 4), q = tid & 3;
+      const int tok = token(tid, n);
       const unsigned char* blk = raw + (tok >> 4) * cache_block_bytes(Dh);
       const unsigned char* sp = blk + off_ks(Dh) + (tok & 15) * (Dh / CACHE_GROUP) + q * (Dh / 64);
       if (Dh == 128) {
@@ -218,19 +222,20 @@ struct KeyPart {
   }
   // [token][channel], K-major: rows of 64 channels (128 bytes), 16-byte chunks exchanged by the row's last three bits
   __device__ __forceinline__ void write(unsigned char* dst, int half, int tid) const {
+    const int q = quarter(tid);
+    unsigned char* at = dst + (q * W >> 3) * ManyPlan<Dh>::SLAB + (half * 64 + token(tid, 0)) * 128;
+    uint32_t place[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) place[i] = (uint32_t)((((q * W + i) & 7) ^ (tid & 7)) << 4);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int row = half * 64 + (tid >> 2) + n * (MANY_CT / 4), q = tid & 3, turn = Dh == 128 ? q & 2 : 0;
-      const __half2 both = k_scales(s[n]), sc = turn ? __lowhigh2highlow(both) : both;
+      const __half2 sc = k_scales(s[n]);
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        // (lanes of the two halves of a row would write to the same banks: those of the second take their words in another order)
-        const uint32_t w = turn ? k[n][(i + 2) % W] : k[n][i];
         const __half2 ss = Dh == 128 && i >= W / 2 ? __high2half2(sc) : __low2half2(sc);
         uint32_t x[4];
-        unpack8(w, ss, __hmul2(ss, __float2half2_rn(-1032.f)), __hmul2(ss, __float2half2_rn(-72.f)), x);
-        const int chunk = q * W + (i ^ turn);   // of eight channels
-        *reinterpret_cast<uint4*>(dst + (chunk >> 3) * ManyPlan<Dh>::SLAB + row * 128 + (((chunk & 7) ^ (row & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+        unpack8(k[n][i], ss, __hmul2(ss, __float2half2_rn(-1032.f)), __hmul2(ss, __float2half2_rn(-72.f)), x);
+        *reinterpret_cast<uint4*>(at + n * (MANY_CT / 4) * 128 + place[i]) = make_uint4(x[0], x[1], x[2], x[3]);
       }
     }
   }
