@@ -346,25 +346,31 @@ __device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* sme
 #pragma unroll 1
     for (int i = 0; i < ops + 2; ++i) {
       const int g = i & 1;
+      // What the two products need besides the weights is waited for first: a wait that finds its barrier complete still takes
+      // 200 cycles, and from the weights on everything waits for the products.
+      const int jv = base + (s.two ? (i - 2) >> 1 : i - 2), sv = jv & 1, jk = base + (s.two ? i >> 1 : i), sk = jk & 1;
+      if (i >= 2 && !mbar_wait(&sh.bars.v_full[sv], (jv >> 1) & 1u, abort, nullptr, a.limit)) return;
+      if (i < 2 && i < ops && !mbar_wait(&sh.bars.q_full[g], segments & 1u, abort, nullptr, a.limit)) return;
+      if (s.two && i < ops && !mbar_wait(&sh.bars.k_full[sk], (jk >> 1) & 1u, abort, nullptr, a.limit)) return;
       if (i >= 2) {
-        const int gj = base + (s.two ? (i - 2) >> 1 : i - 2), st = gj & 1;
         if (!mbar_wait(&sh.bars.p_full[g], weights >> g & 1u, abort, nullptr, a.limit)) return;
         weights ^= 1u << g;
-        if (!mbar_wait(&sh.bars.v_full[st], (gj >> 1) & 1u, abort, nullptr, a.limit)) return;
-        tc_fence_after();
-        const uint64_t b = vd + (uint64_t)(st * (P::TILE >> 4));
+      }
+      tc_fence_after();
+      if (i >= 2) {
+        const uint64_t b = vd + (uint64_t)(sv * (P::TILE >> 4));
         const uint32_t more = i >= 4 ? 1u : 0u, o_at = P::O + g * Dh, s_at = g * 128;
 #pragma unroll
         for (int ks = 0; ks < MANY_TOKENS / 16; ++ks) mma_tmem_a(o_at, s_at + (ks >> 2) * 64 + (ks & 3) * 8, b + (uint64_t)(ks * 128), id_o, ks > 0 ? 1u : more);
         mma_commit(&sh.bars.o_full[g]);
-        mma_commit(&sh.bars.v_free[g][st]);
+        mma_commit(&sh.bars.v_free[g][sv]);
       }
       if (i < ops) {
-        const int gj = base + (s.two ? i >> 1 : i), st = gj & 1;
-        if (i < 2 && !mbar_wait(&sh.bars.q_full[g], segments & 1u, abort, nullptr, a.limit)) return;
-        if (!mbar_wait(&sh.bars.k_full[st], (gj >> 1) & 1u, abort, nullptr, a.limit)) return;
-        tc_fence_after();
-        const uint64_t b = kd + (uint64_t)(st * (P::TILE >> 4)), qa = qd + (uint64_t)(s.two && g ? P::TILE >> 4 : 0);
+        if (!s.two) {   // (a step's keys are used once here, and not always there in time)
+          if (!mbar_wait(&sh.bars.k_full[sk], (jk >> 1) & 1u, abort, nullptr, a.limit)) return;
+          tc_fence_after();
+        }
+        const uint64_t b = kd + (uint64_t)(sk * (P::TILE >> 4)), qa = qd + (uint64_t)(s.two && g ? P::TILE >> 4 : 0);
 #pragma unroll
         for (int ks = 0; ks < Dh / 16; ++ks) {
           constexpr uint64_t step = P::SLAB >> 4;
@@ -372,7 +378,7 @@ __device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* sme
           mma_bf16(g * 128, qa + off, b + off, id_s, ks > 0 ? 1u : 0u);
         }
         mma_commit(&sh.bars.s_full[g]);
-        mma_commit(&sh.bars.k_free[g][st]);
+        mma_commit(&sh.bars.k_free[g][sk]);
       }
     }
     base += s.n;
