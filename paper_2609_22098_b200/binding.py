@@ -116,33 +116,49 @@ class CacheLayout:
         self.dtype = dtype
         self.c = TsCacheLayout(Hq, Hkv, Dh, page_size, n_pages, max_pages, DTYPE_BF16 if dtype == torch.bfloat16 else DTYPE_F32,
                                k_exp, v_exp)
-        self.layer_bytes = int(load_library().ts_cache_bytes(C.byref(self.c)))   # 0: not supported; every call says why
+        self.ref = C.byref(self.c)
+        self.layer_bytes = int(load_library().ts_cache_bytes(self.ref))   # 0: not supported; every call says why
+        self._pool_shape = (n_pages, Hkv, page_size // 16, 18 * Dh)
 
     def pool_shape(self):
         """Shape of one layer's pool (uint8)."""
-        return (self.n_pages, self.Hkv, self.page_size // 16, 18 * self.Dh)
+        return self._pool_shape
 
 
-def _rows_of(t: torch.Tensor, heads: int, Dh: int, dtype, device, what: str):
+def _rows_of(t: torch.Tensor, heads: int, Dh: int, dtype, index: int, what: str):
     """(rows, elements between rows) of a tensor [..., heads, Dh] whose leading dimensions are evenly spaced rows."""
-    if t.dtype != dtype or t.device != device or t.dim() < 3 or t.shape[-2:] != (heads, Dh):
-        raise TreeSparkError(f"{what}: expected {dtype} [..., {heads}, {Dh}] on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.stride(-1) != 1 or (heads > 1 and t.stride(-2) != Dh):
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not dtype or t.get_device() != index or len(shape) < 3 or shape[-1] != Dh or shape[-2] != heads:
+        raise TreeSparkError(f"{what}: expected {dtype} [..., {heads}, {Dh}] on device {index}, got {t.dtype} {tuple(shape)} on {t.device}")
+    if stride[-1] != 1 or (heads > 1 and stride[-2] != Dh):
         raise TreeSparkError(f"{what}: the {heads} heads of a row must be contiguous")
     ld, rows = 0, 1
-    for n, st in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+    for i in range(len(shape) - 3, -1, -1):
+        n = shape[i]
         if n > 1:
             if rows == 1:
-                ld = st
-            elif st != ld * rows:
+                ld = stride[i]
+            elif stride[i] != ld * rows:
                 raise TreeSparkError(f"{what}: rows must be evenly spaced")
         rows *= n
     return rows, ld if rows > 1 else heads * Dh
 
 
-def _check(t: Optional[torch.Tensor], shape, dtype, device, what: str):
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous()):
-        raise TreeSparkError(f"{what}: expected contiguous {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _check(index: int, what: str, *tensors):
+    """Refuses tensors (given as tensor, shape, dtype, name) that the library cannot take as they are; returns their addresses."""
+    at = []
+    for t, shape, dtype, name in tensors:
+        if t is None:
+            at.append(None)
+            continue
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+            raise TreeSparkError(f"{what}: {name}: expected contiguous {dtype} {tuple(shape)} on device {index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        at.append(t.data_ptr())
+    return at
+
+
+_I32 = torch.int32
+_raw_stream = torch._C._cuda_getCurrentRawStream   # torch.cuda.current_stream(i).cuda_stream without the object (1.2 us)
 
 
 class TreeSpark:
@@ -315,27 +331,24 @@ class TreeSpark:
 
     # -- the 4-bit key/value cache --------------------------------------------------------------------
     def _cache_call(self, fn, *args):
-        with torch.cuda.device(self.device):   # the stream is the current one of the context's device
-            self._check(fn(self._ctx, *args, _stream()))
+        index = self._index()
+        if torch.cuda.current_device() == index:   # (the guard alone takes as long as a launch)
+            code = fn(self._ctx, *args, _raw_stream(index))
+        else:
+            with torch.cuda.device(index):
+                code = fn(self._ctx, *args, _raw_stream(index))
+        if code != TS_OK:
+            self._check(code)
 
-    def _pool_check(self, lay, pool, what, layers=False):
-        shape = lay.pool_shape()
-        if pool.dtype != torch.uint8 or pool.device != self._dev() or not pool.is_contiguous() or tuple(pool.shape[-4:]) != shape or \
-                pool.dim() not in ((4, 5) if layers else (4,)):
-            raise TreeSparkError(f"{what}: expected a contiguous uint8 pool {'[layers, ' if layers else '['}{shape}] on {self._dev()}, "
-                                 f"got {pool.dtype} {tuple(pool.shape)} on {pool.device}")
-
-    def _dev(self):
-        if self.device.index is None:
-            self.device = torch.device(self.device.type, self.ws.device.index)
-        return self.device
+    def _index(self):
+        return self.ws.get_device()
 
     def _row_capacity(self, n_nodes):
         return 1 if n_nodes is None else self.Nmax + 1
 
     def alloc_cache(self, lay: CacheLayout, layers: int, B: int) -> Dict[str, torch.Tensor]:
         """An empty cache for ``B`` requests: pool of all layers, block table, pages held, free list, lengths (0)."""
-        d = self._dev()
+        d = self.device
         i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device=d)
         return dict(pool=torch.zeros(layers, *lay.pool_shape(), dtype=torch.uint8, device=d),
                     block_table=torch.full((B, lay.max_pages), -1, dtype=torch.int32, device=d), held=i32(B),
@@ -345,67 +358,63 @@ class TreeSpark:
     def cache_reserve(self, lay, seq_len, held, free_pages, free_count, block_table, n_nodes=None, out=None):
         """Pages and slots for a round's rows.  Returns dict(held, free_count, slot_map, status); without ``out`` the counts
         are updated in place.  ``seq_len`` < 0 gives a request's pages back."""
-        B, d, R = int(seq_len.numel()), self._dev(), self._row_capacity(n_nodes)
+        B, R = seq_len.shape[0], self._row_capacity(n_nodes)
         if out is None:
-            out = dict(held=held, free_count=free_count, slot_map=torch.empty(B, R, dtype=torch.int32, device=d),
-                       status=torch.empty(B, dtype=torch.int32, device=d))
-        for t, shape, what in ((seq_len, (B,), "seq_len"), (held, (B,), "held"), (free_pages, (lay.n_pages,), "free_pages"), (free_count, (1,), "free_count"),
-                               (block_table, (B, lay.max_pages), "block_table"), (n_nodes, (B,), "n_nodes"), (out["held"], (B,), "out held"),
-                               (out["free_count"], (1,), "out free_count"), (out["slot_map"], (B, R), "out slot_map"), (out["status"], (B,), "out status")):
-            _check(t, shape, torch.int32, d, "cache_reserve: " + what)
-        self._cache_call(self.lib.ts_cache_reserve, C.byref(lay.c), B, _ptr(seq_len), _ptr(n_nodes), _ptr(held), _ptr(free_pages), _ptr(free_count),
-                         _ptr(block_table), _ptr(out["held"]), _ptr(out["free_count"]), _ptr(out["slot_map"]), _ptr(out["status"]))
+            out = dict(held=held, free_count=free_count, slot_map=torch.empty(B, R, dtype=torch.int32, device=self.device),
+                       status=torch.empty(B, dtype=torch.int32, device=self.device))
+        each, one = (B,), (1,)
+        at = _check(self._index(), "cache_reserve", (seq_len, each, _I32, "seq_len"), (n_nodes, each, _I32, "n_nodes"), (held, each, _I32, "held"),
+                    (free_pages, (lay.n_pages,), _I32, "free_pages"), (free_count, one, _I32, "free_count"), (block_table, (B, lay.max_pages), _I32, "block_table"),
+                    (out["held"], each, _I32, "out held"), (out["free_count"], one, _I32, "out free_count"), (out["slot_map"], (B, R), _I32, "out slot_map"),
+                    (out["status"], each, _I32, "out status"))
+        self._cache_call(self.lib.ts_cache_reserve, lay.ref, B, *at)
         return out
 
     def cache_append(self, lay, k, v, slot_map, pool, k_val=None, v_val=None):
         """Keys and values [..., Hkv, Dh] into their slots of a layer's ``pool``; ``k_val`` / ``v_val``: what the cache holds for them."""
-        d = self._dev()
-        rows, ldk = _rows_of(k, lay.Hkv, lay.Dh, lay.dtype, d, "cache_append: k")
-        rows_v, ldv = _rows_of(v, lay.Hkv, lay.Dh, lay.dtype, d, "cache_append: v")
+        index = self._index()
+        rows, ldk = _rows_of(k, lay.Hkv, lay.Dh, lay.dtype, index, "cache_append: k")
+        rows_v, ldv = _rows_of(v, lay.Hkv, lay.Dh, lay.dtype, index, "cache_append: v")
         if rows != rows_v or slot_map.numel() != rows:
             raise TreeSparkError(f"cache_append: {rows} rows of k, {rows_v} of v, {slot_map.numel()} slots")
-        _check(slot_map, slot_map.shape, torch.int32, d, "cache_append: slot_map")
-        self._pool_check(lay, pool, "cache_append")
-        for t, what in ((k_val, "k_val"), (v_val, "v_val")):
-            _check(t, k.shape, lay.dtype, d, "cache_append: " + what)
-        self._cache_call(self.lib.ts_cache_append, C.byref(lay.c), rows, _ptr(k), ldk, _ptr(v), ldv, _ptr(slot_map), _ptr(pool), _ptr(k_val), _ptr(v_val))
+        at = _check(index, "cache_append", (slot_map, slot_map.shape, _I32, "slot_map"), (pool, lay._pool_shape, torch.uint8, "pool"),
+                    (k_val, k.shape, lay.dtype, "k_val"), (v_val, v.shape, lay.dtype, "v_val"))
+        self._cache_call(self.lib.ts_cache_append, lay.ref, rows, k.data_ptr(), ldk, v.data_ptr(), ldv, *at)
 
     def attention_workspace(self, lay, B):
         """Workspace of ``tree_attention``.  Calls that may overlap on the GPU (other streams, replayed graphs) need one each."""
-        return torch.empty(max(16, int(self.lib.ts_tree_attention_workspace_bytes(self._ctx, C.byref(lay.c), int(B)))), dtype=torch.uint8, device=self._dev())
+        return torch.empty(max(16, int(self.lib.ts_tree_attention_workspace_bytes(self._ctx, lay.ref, int(B)))), dtype=torch.uint8, device=self.device)
 
     def tree_attention(self, lay, q, pool, block_table, seq_len, n_nodes=None, mask=None, scale=None, out=None, lse=None, ws=None):
         """Attention of a round's rows [B, rows, Hq, Dh] over a layer's cache; ``scale`` defaults to Dh ** -0.5.  Without ``out``
         a zeroed tensor is made (unused rows are never written)."""
-        B, d, R = int(seq_len.numel()), self._dev(), self._row_capacity(n_nodes)
-        rows, ldq = _rows_of(q, lay.Hq, lay.Dh, lay.dtype, d, "tree_attention: q")
-        out = torch.zeros(q.shape, dtype=lay.dtype, device=d) if out is None else out
-        rows_o, ldo = _rows_of(out, lay.Hq, lay.Dh, lay.dtype, d, "tree_attention: out")
-        if rows != B * R or rows_o != B * R:
+        B, R, index = seq_len.shape[0], self._row_capacity(n_nodes), self._index()
+        rows, ldq = _rows_of(q, lay.Hq, lay.Dh, lay.dtype, index, "tree_attention: q")
+        out = torch.zeros(q.shape, dtype=lay.dtype, device=q.device) if out is None else out
+        rows_o, ldo = _rows_of(out, lay.Hq, lay.Dh, lay.dtype, index, "tree_attention: out")
+        if rows != B * R or rows_o != rows:
             raise TreeSparkError(f"tree_attention: {B} requests of {R} rows, but q has {rows} and out {rows_o}")
-        for t, shape, what in ((seq_len, (B,), "seq_len"), (block_table, (B, lay.max_pages), "block_table"), (n_nodes, (B,), "n_nodes")):
-            _check(t, shape, torch.int32, d, "tree_attention: " + what)
-        _check(mask, (B, self.Nmax, self.words), torch.int64, d, "tree_attention: mask")
-        self._pool_check(lay, pool, "tree_attention")
         if lse is not None and lse.numel() != rows * lay.Hq:
             raise TreeSparkError(f"tree_attention: lse must have {rows * lay.Hq} elements")
-        _check(lse, () if lse is None else lse.shape, torch.float32, d, "tree_attention: lse")
         ws = self.attention_workspace(lay, B) if ws is None else ws
-        self._cache_call(self.lib.ts_tree_attention, C.byref(lay.c), B, _ptr(q), ldq, _ptr(pool), _ptr(block_table), _ptr(seq_len), _ptr(n_nodes), _ptr(mask),
-                         float(lay.Dh ** -0.5 if scale is None else scale), _ptr(out), ldo, _ptr(lse), _ptr(ws), ws.numel())
+        p_pool, p_table, p_len, p_nodes, p_mask, p_lse, p_ws = _check(
+            index, "tree_attention", (pool, lay._pool_shape, torch.uint8, "pool"), (block_table, (B, lay.max_pages), _I32, "block_table"), (seq_len, (B,), _I32, "seq_len"),
+            (n_nodes, (B,), _I32, "n_nodes"), (mask, (B, self.Nmax, self.words), torch.int64, "mask"), (lse, None if lse is None else lse.shape, torch.float32, "lse"),
+            (ws, ws.shape, torch.uint8, "ws"))
+        self._cache_call(self.lib.ts_tree_attention, lay.ref, B, q.data_ptr(), ldq, p_pool, p_table, p_len, p_nodes, p_mask, lay.Dh ** -0.5 if scale is None else scale,
+                         out.data_ptr(), ldo, p_lse, p_ws, ws.numel())
         return out
 
     def cache_commit(self, lay, pool, block_table, seq_len, acc_len, acc_node, seq_len_out=None):
         """Move the accepted paths' rows to the ends of the prefixes, in all layers of ``pool`` ([layers, ...] or one layer);
         returns the new lengths (in place without ``seq_len_out``)."""
-        B, d = int(seq_len.numel()), self._dev()
+        B = seq_len.shape[0]
         seq_len_out = seq_len if seq_len_out is None else seq_len_out
-        self._pool_check(lay, pool, "cache_commit", layers=True)
-        for t, shape, what in ((seq_len, (B,), "seq_len"), (block_table, (B, lay.max_pages), "block_table"), (acc_len, (B,), "acc_len"),
-                               (acc_node, (B, self.D), "acc_node"), (seq_len_out, (B,), "seq_len_out")):
-            _check(t, shape, torch.int32, d, "cache_commit: " + what)
-        self._cache_call(self.lib.ts_cache_commit, C.byref(lay.c), B, pool.shape[0] if pool.dim() == 5 else 1, lay.layer_bytes, _ptr(pool), _ptr(block_table),
-                         _ptr(seq_len), _ptr(acc_len), _ptr(acc_node), _ptr(seq_len_out))
+        layers = pool.shape[0] if pool.dim() == 5 else 1
+        shape = (layers, *lay._pool_shape) if pool.dim() == 5 else lay._pool_shape
+        at = _check(self._index(), "cache_commit", (pool, shape, torch.uint8, "pool"), (block_table, (B, lay.max_pages), _I32, "block_table"), (seq_len, (B,), _I32, "seq_len"),
+                    (acc_len, (B,), _I32, "acc_len"), (acc_node, (B, self.D), _I32, "acc_node"), (seq_len_out, (B,), _I32, "seq_len_out"))
+        self._cache_call(self.lib.ts_cache_commit, lay.ref, B, layers, lay.layer_bytes, *at)
         return seq_len_out
 
     def verify_tree(self, U, A, W, Z, z_row_off, anchor_tok, tree, T, seed, out=None, edge_stat=True):

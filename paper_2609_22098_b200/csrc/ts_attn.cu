@@ -12,7 +12,7 @@ namespace ts {
 // ------------------------------------------------------------------------------------------------
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
-constexpr int FEW_BLOCKS = 2;                        // blocks a warp takes in a step: two score chains side by side
+constexpr int FEW_BLOCKS = 3;                        // blocks a warp takes in a step: what a step costs besides them is shared, their chains run side by side
 constexpr int FEW_TOKENS = FEW_BLOCKS * CACHE_BLOCK;
 template <int NT> using FewShape = AttnShape<8 * NT, FEW_TOKENS, 1, 1>;
 
@@ -21,7 +21,7 @@ struct FewPlan {
   static constexpr int QT = 8 * NT;
   static constexpr int BLK = cache_block_bytes(Dh);
   static constexpr int STEP = FEW_BLOCKS * BLK;
-  static constexpr int STAGES = 3;
+  static constexpr int STAGES = 2;
   static constexpr int ROW = Dh + 4;                       // floats between rows of the merge buffer
   static constexpr int RING = FEW_WARPS * STAGES * STEP;
   static constexpr int MERGE = FEW_WARPS * QT * (ROW + 2) * 4;
@@ -43,7 +43,8 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
 
 // The query rows of a unit as B operands: lane (g, t) holds channels t Dh/4 .. of row g of each tile of eight.  A row is
 // multiplied by the power of two that brings its largest element to 2^14..2^15: bf16 then is exact in fp16 down to 2^-38 of
-// that element.  fp32 is split into two fp16 parts, exact to 2^-22.  f: what a column's scores are multiplied with.
+// that element.  fp32 is split into two fp16 parts, exact to 2^-22.  The scale's sign goes to the queries, its magnitude to f: what
+// a column's sums are multiplied with (not 0, so that a masked sum, -inf, has weight 0 whatever the scale is).
 template <int Dh, int NT, bool F32>
 struct Queries {
   static constexpr int REGS = Dh / 8;   // registers a tile
@@ -81,7 +82,7 @@ struct Queries {
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
       const int e = max((int)(__float_as_uint(top) >> 23), 20);         // biased exponent; 2^(141 - e) has to be a float
-      const float up = __uint_as_float((unsigned)(127 + 141 - e) << 23), mine = a.qk * __uint_as_float((unsigned)(127 + e - 141) << 23);
+      const float up = copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk), mine = fmaxf(1e-30f, fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23));
 #pragma unroll
       for (int i = 0; i < REGS; ++i) {
         const float x0 = x[2 * i] * up, x1 = x[2 * i + 1] * up;
@@ -225,7 +226,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
   const int per = a.d.ps / CACHE_BLOCK, adv = FEW_WARPS * FEW_BLOCKS, adv_c = adv / per, adv_in = adv - adv_c * per;
   AttnUnit fu = u;
   int fj = (int)(start - u.t0) + w, fleft = (int)(end - start) - w, fc = fj * FEW_BLOCKS / per, fin = fj * FEW_BLOCKS - fc * per, fh = fu.v / fu.nq;
-  int fslot = 0, copies = 0, page0 = -1, page1 = -1;
+  int fslot = 0, copies = 0, page = -1, inner = 0;   // (lanes 0 and 1: a block each)
   auto look_up = [&]() {
     if (fleft <= 0) return;
     if (fj >= fu.n) {
@@ -235,22 +236,23 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
       } while (fj >= fu.n);
       fc = fj * FEW_BLOCKS / per; fin = fj * FEW_BLOCKS - fc * per; fh = fu.v / fu.nq;
     }
-    const int* row = a.table + (size_t)fu.b * a.d.cols;
-    const int c1 = fin + 1 < per ? fc : fc + 1;
+    inner = fin + lane;
+    int c = fc;
+    while (inner >= per) { inner -= per; ++c; }
     const unsigned last = (unsigned)fu.seq + (unsigned)fu.rows - 1u;   // the request's last token; a block behind it is not fetched
-    page0 = fc < a.d.cols ? __ldg(row + fc) : -1;
-    page1 = c1 < a.d.cols && (unsigned)(fj * FEW_BLOCKS + 1) * CACHE_BLOCK <= last ? __ldg(row + c1) : -1;
+    page = lane < FEW_BLOCKS && c < a.d.cols && (unsigned)(fj * FEW_BLOCKS + lane) * CACHE_BLOCK <= last ? __ldg(a.table + (size_t)fu.b * a.d.cols + c) : -1;
   };
   auto fetch = [&]() {
     if (fleft <= 0) return;
+    const long long off = block_offset(a.d, page, inner, fh);
+    const unsigned there = __ballot_sync(~0u, off >= 0);
+    uint64_t* bar = &bars[w][fslot];
     if (lane == 0) {
-      const long long off0 = block_offset(a.d, page0, fin, fh), off1 = block_offset(a.d, page1, fin + 1 < per ? fin + 1 : 0, fh);
-      present[w][fslot] = (off0 >= 0 ? 1 : 0) | (off1 >= 0 ? 2 : 0);
-      uint64_t* bar = &bars[w][fslot];
-      mbar_expect_tx(bar, (off0 >= 0 ? BLK : 0) + (off1 >= 0 ? BLK : 0));
-      if (off0 >= 0) bulk_load(ring + fslot * P::STEP, a.pool + off0, BLK, bar);
-      if (off1 >= 0) bulk_load(ring + fslot * P::STEP + BLK, a.pool + off1, BLK, bar);
+      present[w][fslot] = (int)there;
+      mbar_expect_tx(bar, __popc(there) * BLK);
     }
+    __syncwarp();
+    if (off >= 0) bulk_load(ring + fslot * P::STEP + lane * BLK, a.pool + off, BLK, bar);
     ++copies;
     if (++fslot == ST) fslot = 0;
     fj += FEW_WARPS; fleft -= FEW_WARPS;
@@ -295,10 +297,6 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
       uint32_t ph[FEW_BLOCKS][NT][2], pl[FEW_BLOCKS][F32 ? NT : 1][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int k = 0; k < FEW_BLOCKS; ++k)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) s[k][n][c] *= q.f[n][c & 1];
         if (masked) {
 #pragma unroll
           for (int k = 0; k < FEW_BLOCKS; ++k)
@@ -318,6 +316,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
           top[c] = fmaxf(s[0][n][c], s[0][n][c + 2]);
 #pragma unroll
           for (int k = 1; k < FEW_BLOCKS; ++k) top[c] = fmaxf(top[c], fmaxf(s[k][n][c], s[k][n][c + 2]));
+          top[c] *= q.f[n][c];
         }
         if (__any_sync(~0u, top[0] > m[n][0] || top[1] > m[n][1])) {
 #pragma unroll
@@ -337,7 +336,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
         for (int k = 0; k < FEW_BLOCKS; ++k) {
           float e[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) e[c] = ex2(s[k][n][c] - ref[n][c & 1]);
+          for (int c = 0; c < 4; ++c) e[c] = ex2(fmaf(s[k][n][c], q.f[n][c & 1], -ref[n][c & 1]));
           l[n][0] += e[0] + e[2]; l[n][1] += e[1] + e[3];
           const __half2 h0 = __floats2half2_rn(e[0], e[1]), h1 = __floats2half2_rn(e[2], e[3]);
           ph[k][n][0] = transpose8(as_u32(h0)); ph[k][n][1] = transpose8(as_u32(h1));

@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
 // Commit.  A warp per (request, layer, head) holds the bytes of all moved rows before it writes one: sources and targets of
 // a path overlap.  The CTAs of a request form a cluster, whose barrier lets the new length overwrite the old.
 // ------------------------------------------------------------------------------------------------
-constexpr int COM_THREADS = 256;
+constexpr int COM_THREADS = 1024;   // (a single request: 256 warps, one round for 32 layers of eight heads)
 constexpr int COM_CLUSTER = 8;
 
 struct CommitArgs {
@@ -373,7 +373,7 @@ struct CommitArgs {
 };
 
 template <int Dh>
-__global__ void __launch_bounds__(COM_THREADS) commit_kernel(const CommitArgs a) {
+__global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs a) {
   constexpr int G = Dh / CACHE_GROUP;
   __shared__ long long from[DMAX], to[DMAX];   // byte offsets of the rows' blocks in layer 0, head 0; -1: no move
   __shared__ int ft[DMAX], tt[DMAX];           // tokens within the blocks
@@ -406,7 +406,9 @@ __global__ void __launch_bounds__(COM_THREADS) commit_kernel(const CommitArgs a)
     const int layer = item / a.d.Hkv, h = item - layer * a.d.Hkv;
     unsigned char* base = a.pool + (size_t)layer * a.layer_stride + (size_t)h * (a.d.ps / CACHE_BLOCK) * cache_block_bytes(Dh);
     uint32_t word[DMAX];
-    unsigned char byte[DMAX];
+    uint32_t byte[DMAX / 4];   // (packed: 1,024 threads have 64 registers each)
+#pragma unroll
+    for (int i = 0; i < DMAX / 4; ++i) byte[i] = 0u;
     const int j = lane % W;
     const bool has_word = lane < 2 * W, has_byte = lane < 2 * G;
     auto word_at = [&](unsigned char* blk, int tau) {
@@ -419,14 +421,14 @@ __global__ void __launch_bounds__(COM_THREADS) commit_kernel(const CommitArgs a)
     for (int i = 0; i < DMAX; ++i)
       if (i < n && from[i] >= 0) {
         if (has_word) word[i] = *word_at(base + from[i], ft[i]);
-        if (has_byte) byte[i] = *byte_at(base + from[i], ft[i]);
+        if (has_byte) byte[i / 4] |= (uint32_t)*byte_at(base + from[i], ft[i]) << (8 * (i % 4));
       }
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < DMAX; ++i)
       if (i < n && from[i] >= 0) {
         if (has_word) *word_at(base + to[i], tt[i]) = word[i];
-        if (has_byte) *byte_at(base + to[i], tt[i]) = byte[i];
+        if (has_byte) *byte_at(base + to[i], tt[i]) = (unsigned char)(byte[i / 4] >> (8 * (i % 4)));
       }
     __syncwarp();
   }
