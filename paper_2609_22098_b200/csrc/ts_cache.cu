@@ -40,7 +40,7 @@ bool on_ctx_device(const ts_ctx* ctx) {
 
 // ------------------------------------------------------------------------------------------------
 // Reserve.  Every CTA adds up the pages that all requests need (a few thousand at most), then serves its share of the
-// requests, one warp each.  The calls that fit are one launch of a cluster of eight CTAs whose barrier separates reading the
+// requests, one warp each (and all of its warps for the many entries of a request that starts).  The calls that fit are one launch of a cluster of eight CTAs whose barrier separates reading the
 // counts from writing them, so that they may be updated in place; where whole tables are written, many CTAs write them and a
 // second launch updates the counts.
 // ------------------------------------------------------------------------------------------------
@@ -123,11 +123,12 @@ __device__ __forceinline__ ReservePlan plan_of(const ReserveArgs& a, int b, long
   return p;
 }
 
-// one warp: the request's new table entries and the slots of its rows
+// one warp: the slots of a request's rows and its new table entries, or the first of them where they are many
+constexpr int RES_SHORT = 64;   // entries of a request that its warp writes; what is more is written by the whole CTA
 __device__ void reserve_rows(const ReserveArgs& a, int b, const ReservePlan& p, int count, int lane) {
   int* row = a.table + (size_t)b * a.d.cols;
   if (p.granted)
-    for (int c = p.held + lane; c < p.need; c += 32) row[c] = a.free_pages[count - 1 - (p.start + c - p.held)];
+    for (int c = p.held + lane; c < min(p.need, p.held + RES_SHORT); c += 32) row[c] = a.free_pages[count - 1 - (p.start + c - p.held)];
   const int first = a.seq_len[b];
   for (int i = lane; i < a.rcap; i += 32) {
     int slot = -1;
@@ -139,6 +140,21 @@ __device__ void reserve_rows(const ReserveArgs& a, int b, const ReservePlan& p, 
     a.slot_map[(size_t)b * a.rcap + i] = slot;
   }
   if (lane == 0) a.status[b] = p.release || p.granted ? TS_OK : TS_ERR_OVERFLOW;
+}
+
+// a CTA's requests (every gridDim.x-th): a warp each, then the long ones by all threads
+__device__ void reserve_tables(const ReserveArgs& a, const long long* pre, int count) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, step = gridDim.x;
+  for (int b = blockIdx.x + warp * step; b < a.B; b += RES_THREADS / 32 * step) reserve_rows(a, b, plan_of(a, b, pre[b], count), count, lane);
+  if (a.d.cols <= RES_SHORT) return;
+  for (int b = blockIdx.x; b < a.B; b += step) {
+    if (pages_taken(a, b) <= RES_SHORT) continue;
+    const ReservePlan p = plan_of(a, b, pre[b], count);
+    if (!p.granted) continue;
+    int* row = a.table + (size_t)b * a.d.cols;
+#pragma unroll 4
+    for (int c = p.held + RES_SHORT + threadIdx.x; c < p.need; c += RES_THREADS) row[c] = a.free_pages[count - 1 - (p.start + c - p.held)];
+  }
 }
 
 // The last request that got pages ends at this many (the running sum does not fall, so those that got some come first).
@@ -172,8 +188,7 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
     constexpr int OWN = RES_MAX_B / RES_THREADS;
     int new_held[OWN];
     const int warps = (WHERE == 0 ? RES_CLUSTER : 1) * (RES_THREADS / 32), me = blockIdx.x * (RES_THREADS / 32) + (threadIdx.x >> 5);
-    if (WHERE == 0)
-      for (int b = me; b < a.B; b += warps) reserve_rows(a, b, plan_of(a, b, pre[b], count), count, lane);
+    if (WHERE == 0) reserve_tables(a, pre, count);
     if (blockIdx.x == 0) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
@@ -210,9 +225,7 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
       if (threadIdx.x == 0) a.free_count_out[0] = min(base + (int)(all >> 32), a.d.n_pages);
     }
   } else {
-    const int warps = gridDim.x * (RES_THREADS / 32);
-    for (int b = blockIdx.x * (RES_THREADS / 32) + (threadIdx.x >> 5); b < a.B; b += warps)
-      reserve_rows(a, b, plan_of(a, b, pre[b], count), count, lane);
+    reserve_tables(a, pre, count);
   }
 }
 
@@ -232,7 +245,7 @@ static cudaError_t launch_reserve(ts_ctx* ctx, const ReserveArgs& a, cudaStream_
   cudaError_t e;
   {
     ProfScope ps(ctx, K_RESERVE, st);
-    const int grid = (int)std::min<long long>(((long long)a.B + RES_THREADS / 32 - 1) / (RES_THREADS / 32), 2 * ctx->num_sms);
+    const int grid = std::min(a.B, 2 * ctx->num_sms);
     e = launch_kernel(reserve_kernel<1>, dim3(grid), dim3(RES_THREADS), smem, st, true, a);
   }
   if (e != cudaSuccess) return e;
@@ -360,7 +373,7 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
 // Commit.  A warp per (request, layer, head) holds the bytes of all moved rows before it writes one: sources and targets of
 // a path overlap.  The CTAs of a request form a cluster, whose barrier lets the new length overwrite the old.
 // ------------------------------------------------------------------------------------------------
-constexpr int COM_THREADS = 1024;   // (a single request: 256 warps, one round for 32 layers of eight heads)
+constexpr int COM_THREADS = 1024;   // at most: a warp for each layer and head of a request where 256 are enough
 constexpr int COM_CLUSTER = 8;
 
 struct CommitArgs {
@@ -401,8 +414,8 @@ __global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs
   __syncthreads();
   // a lane's word of a token: K codes, then V codes; its byte: K scales, then V scales
   constexpr int W = Dh / 8;   // words of K codes (as many of V)
-  const int warps = COM_CLUSTER * (COM_THREADS / 32);
-  for (int item = part * (COM_THREADS / 32) + (threadIdx.x >> 5); item < a.layers * a.d.Hkv; item += warps) {
+  const int warps = COM_CLUSTER * (blockDim.x / 32);
+  for (int item = part * (blockDim.x / 32) + (threadIdx.x >> 5); item < a.layers * a.d.Hkv; item += warps) {
     const int layer = item / a.d.Hkv, h = item - layer * a.d.Hkv;
     unsigned char* base = a.pool + (size_t)layer * a.layer_stride + (size_t)h * (a.d.ps / CACHE_BLOCK) * cache_block_bytes(Dh);
     uint32_t word[DMAX];
@@ -522,7 +535,7 @@ extern "C" int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* lay, int3
   {
     ProfScope ps(ctx, K_COMMIT, st);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(B * COM_CLUSTER); cfg.blockDim = dim3(COM_THREADS); cfg.stream = st;
+    cfg.gridDim = dim3(B * COM_CLUSTER); cfg.blockDim = dim3(std::min(COM_THREADS, (layers * lay->Hkv + COM_CLUSTER - 1) / COM_CLUSTER * 32)); cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = COM_CLUSTER; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
