@@ -102,7 +102,8 @@ int32_t ts_set_ablation(ts_ctx* ctx, uint32_t flags);
  *   TS_TEST_SHORT_WAITS   bounded waits give up after 4096 polls instead of 2^22
  *   TS_TEST_LOST_ARRIVAL  the grid barriers of the walk and of the tensor-core scoring kernel expect one
  *                         arrival more than will come: the waits run out, the kernels return, and the
- *                         requests are reported with TS_ERR_TIMEOUT in status[] (given parents: by NaN) */
+ *                         requests are reported with TS_ERR_TIMEOUT in status[] (given parents: by NaN).  ts_tree_attention
+ *                         expects bytes of its copies that do not come: its rows are NaN */
 #define TS_TEST_FORCE_FMA 1u
 #define TS_TEST_NO_TMA 2u
 #define TS_TEST_NO_FEW 4u

@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
     uint64_t* bar = &bars[w][fslot];
     if (lane == 0) {
       present[w][fslot] = (int)there;
-      mbar_expect_tx(bar, __popc(there) * BLK);
+      mbar_expect_tx(bar, __popc(there) * BLK + a.lost);
     }
     __syncwarp();
     if (off >= 0) bulk_load(ring + fslot * P::STEP + lane * BLK, a.pool + off, BLK, bar);
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
       m[n][0] = m[n][1] = -INFINITY; ref[n][0] = ref[n][1] = 0.f; l[n][0] = l[n][1] = 0.f;
     }
     for (; mine < pos + seg; mine += FEW_WARPS) {
-      const bool ok = mbar_wait(&bars[w][slot], phase, (volatile int*)&gave_up, nullptr, a.limit);
+      const bool ok = __all_sync(~0u, mbar_wait(&bars[w][slot], phase, (volatile int*)&gave_up, nullptr, a.limit));
       const int here = present[w][slot];
       const unsigned char* blk = ring + slot * P::STEP;
       float s[FEW_BLOCKS][NT][4];
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
       for (int k = 0; k < FEW_BLOCKS; ++k) value_block<Dh, NT, F32>(blk + k * BLK, ph[k], pl[k], o, g, t);
       __syncwarp();   // every lane has read the slot that the next copies go to
       if (++slot == ST) { slot = 0; phase ^= 1u; }
-      fetch();
+      if (ok) fetch();   // (a slot whose copies have not come is not used again)
     }
     // ---- the four warps' parts of the unit
 #pragma unroll
@@ -566,7 +566,7 @@ extern "C" int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* lay, in
   a.q = q; a.ldq = ldq; a.pool = (const unsigned char*)pool; a.table = block_table; a.seq_len = seq_len; a.n_nodes = n_nodes; a.mask = mask;
   a.by_g = (unsigned)(((1ull << 32) + a.d.G - 1) / a.d.G);   // (G = 1: not used)
   a.qk = ldexpf(scale * LOG2E, K_SHIFT + lay->k_exp); a.vo = ldexpf(1.f, V_SHIFT + lay->v_exp);
-  a.out = out; a.ldo = ldo; a.lse = lse; a.limit = ctx->wait_limit;
+  a.out = out; a.ldo = ldo; a.lse = lse; a.limit = ctx->wait_limit; a.lost = ctx->test_mode & TS_TEST_LOST_ARRIVAL ? 16u : 0u;
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e = takes_many(a.d, a.rcap, f32) ? attn_many_launch(ctx, a, (char*)ws, st) : attn_few_launch(ctx, a, f32, (char*)ws, st);
   if (e == cudaSuccess) e = cudaGetLastError();

@@ -175,7 +175,7 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
       if (lane == 0) {
         unsigned char* pr = &sh.present[(copied >> 1) % MANY_PRESENT];
         *pr = (unsigned char)((copied & 1) ? *pr | there << 4 : there);
-        mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * BLK);
+        mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * BLK + a.lost);
       }
       __syncwarp();
       if (lane >> 2 == k && now >= 0)
@@ -299,7 +299,7 @@ __device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* r
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
         Part part;
-        if (!mbar_wait(&sh.bars.raw_full[slot], phase, abort, nullptr, a.limit)) return;
+        if (!__all_sync(~0u, mbar_wait(&sh.bars.raw_full[slot], phase, abort, nullptr, a.limit))) return;
         part.read(raw + slot * P::RAW, tid);
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.bars.raw_free[slot]);
@@ -307,7 +307,7 @@ __device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* r
         if (half == 0) {
 #pragma unroll
           for (int g = 0; g < 2; ++g)
-            if (before >> g & 1u && !mbar_wait(&free[g][st], (turn >> (2 * st + g) & 1u) ^ 1u, abort, nullptr, a.limit)) return;
+            if (before >> g & 1u && !__all_sync(~0u, mbar_wait(&free[g][st], (turn >> (2 * st + g) & 1u) ^ 1u, abort, nullptr, a.limit))) return;
         }
         part.write(stages + st * P::TILE, half, tid);
       }

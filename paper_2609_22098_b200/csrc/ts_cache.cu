@@ -40,16 +40,18 @@ bool on_ctx_device(const ts_ctx* ctx) {
 
 // ------------------------------------------------------------------------------------------------
 // Reserve.  Every CTA adds up the pages that all requests need (a few thousand at most), then serves its share of the
-// requests, one warp each (and all of its warps for the many entries of a request that starts).  The calls that fit are one launch of a cluster of eight CTAs whose barrier separates reading the
+// requests, one warp each (and all of its warps for the many entries of a request that starts).  Small calls are one launch of a cluster of eight CTAs whose barrier separates reading the
 // counts from writing them, so that they may be updated in place; where whole tables are written, many CTAs write them and a
 // second launch updates the counts.
 // ------------------------------------------------------------------------------------------------
 constexpr int RES_THREADS = 512;
 constexpr int RES_CLUSTER = 8;
 constexpr int RES_MAX_B = 4096;
-// Above this many table entries (requests times columns, what the host knows) the entries outweigh the second launch.
-// 148 CTAs against a cluster of eight: at the sizes the figures beside launch_reserve name.
-constexpr long long RES_GRID_MIN = 1 << 17;
+// The cluster's form: up to this many requests and table entries (requests times columns, what the host knows).  A round of 32
+// requests with 500 columns takes the cluster 7.6 us and many CTAs 9.1, 32 whole tables of 500 columns 9.7 and 9.4, of 2,000
+// columns 11.7 and 10.3, 128 of 500 columns 20 and 10, 500 of 1,875 columns 94 and 18.
+constexpr int RES_CLUSTER_B = 64;
+constexpr long long RES_CLUSTER_ENTRIES = 1 << 16;
 
 struct ReserveArgs {
   CacheDims d;
@@ -231,7 +233,7 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
 
 static cudaError_t launch_reserve(ts_ctx* ctx, const ReserveArgs& a, cudaStream_t st) {
   const size_t smem = (size_t)a.B * sizeof(long long);
-  if ((long long)a.B * a.d.cols < RES_GRID_MIN) {
+  if (a.B <= RES_CLUSTER_B && (long long)a.B * a.d.cols <= RES_CLUSTER_ENTRIES) {
     ProfScope ps(ctx, K_RESERVE, st);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(RES_CLUSTER); cfg.blockDim = dim3(RES_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
