@@ -103,7 +103,8 @@ int32_t ts_set_ablation(ts_ctx* ctx, uint32_t flags);
  *   TS_TEST_LOST_ARRIVAL  the grid barriers of the walk and of the tensor-core scoring kernel expect one
  *                         arrival more than will come: the waits run out, the kernels return, and the
  *                         requests are reported with TS_ERR_TIMEOUT in status[] (given parents: by NaN).  ts_tree_attention
- *                         expects bytes of its copies that do not come: its rows are NaN */
+ *                         with more than 16 query rows a kv head (bf16) expects bytes of its copies that do not come:
+ *                         its rows are NaN */
 #define TS_TEST_FORCE_FMA 1u
 #define TS_TEST_NO_TMA 2u
 #define TS_TEST_NO_FEW 4u
@@ -408,7 +409,7 @@ int32_t ts_cache_append(ts_ctx* ctx, const ts_cache_layout* layout, int32_t rows
  * page are absent; a row that sees no token gets 0 and lse = -inf.  What stands in the cache behind the last row, or in
  * nodes that a row does not see, does not matter, NaN included.  ws: ts_tree_attention_workspace_bytes() bytes (it does not
  * grow with B or the lengths); calls that overlap on the GPU, replayed graphs among them, need one each.  A bounded
- * device-side wait that runs out gives NaN.
+ * device-side wait that runs out gives NaN (bf16 with more than 16 rows a kv head; the other kernels have no such waits).
  */
 size_t ts_tree_attention_workspace_bytes(const ts_ctx* ctx, const ts_cache_layout* layout, int32_t B);
 int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B, const void* q, int64_t ldq, const void* pool,

@@ -28,12 +28,21 @@ struct FewPlan {
   static constexpr int SMEM = RING + MERGE;
 };
 
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+// A block to shared memory by the warp's lanes, 16 bytes each at a time.  (Bulk copies take as long, and barriers besides.)
+template <int BLK>
+__device__ __forceinline__ void copy_block(uint32_t dst, const unsigned char* src, int lane) {
+#pragma unroll
+  for (int k = 0; k < BLK; k += 512)
+    if (k + 512 <= BLK || k + lane * 16 < BLK) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + k + lane * 16), "l"(src + k + lane * 16) : "memory");
 }
 __device__ __forceinline__ void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// the first product of a sum
+__device__ __forceinline__ void mma_16816_first(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
@@ -100,8 +109,6 @@ struct Queries {
 template <int Dh, int NT, bool F32>
 __device__ __forceinline__ void score_block(const unsigned char* blk, const Queries<Dh, NT, F32>& q, float (&s)[NT][4], int g, int t) {
   constexpr int KW = Dh / 32;        // words of a token's K codes that a lane holds
-#pragma unroll
-  for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
   uint32_t kw[2][KW];
   __half2 sc[2];
 #pragma unroll
@@ -133,14 +140,13 @@ __device__ __forceinline__ void score_block(const unsigned char* blk, const Quer
       for (int n = 0; n < NT; ++n) {
         if (F32) {
           // each step's sum apart and added in fp32: the instruction's own accumulation rounds towards zero
-          float c[4] = {0.f, 0.f, 0.f, 0.f};
-          mma_16816(c, fr, q.lo[F32 ? n : 0][F32 ? r : 0], q.lo[F32 ? n : 0][F32 ? r + 1 : 0]);
+          float c[4];
+          mma_16816_first(c, fr, q.lo[F32 ? n : 0][F32 ? r : 0], q.lo[F32 ? n : 0][F32 ? r + 1 : 0]);
           mma_16816(c, fr, q.hi[n][r], q.hi[n][r + 1]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) s[n][k] += c[k];
-        } else {
-          mma_16816(s[n], fr, q.hi[n][r], q.hi[n][r + 1]);
-        }
+          for (int k = 0; k < 4; ++k) s[n][k] = r == 0 ? c[k] : s[n][k] + c[k];
+        } else if (r == 0) mma_16816_first(s[n], fr, q.hi[n][r], q.hi[n][r + 1]);
+        else mma_16816(s[n], fr, q.hi[n][r], q.hi[n][r + 1]);
       }
     }
   }
@@ -181,8 +187,8 @@ __device__ __forceinline__ void value_block(const unsigned char* blk, const uint
       for (int n = 0; n < NT; ++n) {
         float* acc = o[n][4 * i + j];
         if (F32) {
-          float c[4] = {0.f, 0.f, 0.f, 0.f};
-          mma_16816(c, fr, pl[F32 ? n : 0][0], pl[F32 ? n : 0][1]);
+          float c[4];
+          mma_16816_first(c, fr, pl[F32 ? n : 0][0], pl[F32 ? n : 0][1]);
           mma_16816(c, fr, ph[n][0], ph[n][1]);
 #pragma unroll
           for (int k = 0; k < 4; ++k) acc[k] += c[k];
@@ -202,31 +208,23 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
   constexpr int MT = Dh / 16;        // tiles of 16 channels
   constexpr float ROOM = F32 ? 0.f : 8.f, LIFT = F32 ? 15.f : 7.f;
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ uint64_t bars[FEW_WARPS][ST];
-  __shared__ int present[FEW_WARPS][ST];   // a bit for each block of the step
-  __shared__ int gave_up;
   float* merge = reinterpret_cast<float*>(smem + P::RING);
   float* merge_ml = merge + FEW_WARPS * QT * P::ROW;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  if (threadIdx.x == 0) gave_up = 0;
-  if (lane == 0) {
-#pragma unroll
-    for (int s = 0; s < ST; ++s) mbar_init(&bars[w][s], 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
   pdl_wait();
   pdl_launch_dependents();
   AttnUnit u;
   long long start, end;
   if (!attn_locate<FewShape<NT>, FEW_THREADS>(a, u, start, end)) return;
 
-  // The copies run ahead of the arithmetic, across units: the warp's steps are w, w + 4, .. of the CTA's piece.  The cursor
+  // The copies run ahead of the arithmetic, across units (each warp has a ring and copy groups of its own, nothing waits for another warp): the warp's steps are w, w + 4, .. of the CTA's piece.  The cursor
   // stands at step fj of unit fu, in column fc and block fin of that page; the table's entries are read a step ahead.
   unsigned char* ring = smem + w * ST * P::STEP;
   const int per = a.d.ps / CACHE_BLOCK, adv = FEW_WARPS * FEW_BLOCKS, adv_c = adv / per, adv_in = adv - adv_c * per;
   AttnUnit fu = u;
   int fj = (int)(start - u.t0) + w, fleft = (int)(end - start) - w, fc = fj * FEW_BLOCKS / per, fin = fj * FEW_BLOCKS - fc * per, fh = fu.v / fu.nq;
-  int fslot = 0, copies = 0, page = -1, inner = 0;   // (lanes 0 and 1: a block each)
+  int fslot = 0, page = -1, inner = 0;   // (the first lanes: a block each)
+  uint32_t present = 0;                  // four bits a slot: its blocks that have a page
   auto look_up = [&]() {
     if (fleft <= 0) return;
     if (fj >= fu.n) {
@@ -243,29 +241,29 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
     page = lane < FEW_BLOCKS && c < a.d.cols && (unsigned)(fj * FEW_BLOCKS + lane) * CACHE_BLOCK <= last ? __ldg(a.table + (size_t)fu.b * a.d.cols + c) : -1;
   };
   auto fetch = [&]() {
-    if (fleft <= 0) return;
-    const long long off = block_offset(a.d, page, inner, fh);
-    const unsigned there = __ballot_sync(~0u, off >= 0);
-    uint64_t* bar = &bars[w][fslot];
-    if (lane == 0) {
-      present[w][fslot] = (int)there;
-      mbar_expect_tx(bar, __popc(there) * BLK + a.lost);
+    if (fleft > 0) {
+      const long long off = block_offset(a.d, page, inner, fh);
+      const unsigned there = __ballot_sync(~0u, off >= 0);
+      present = (present & ~(0xFu << (4 * fslot))) | there << (4 * fslot);
+      const uint32_t dst = smem_u32(ring + fslot * P::STEP);
+#pragma unroll
+      for (int k = 0; k < FEW_BLOCKS; ++k) {
+        const long long at = __shfl_sync(~0u, off, k);
+        if (at >= 0) copy_block<BLK>(dst + k * BLK, a.pool + at, lane);
+      }
+      if (++fslot == ST) fslot = 0;
+      fj += FEW_WARPS; fleft -= FEW_WARPS;
+      fc += adv_c; fin += adv_in;
+      if (fin >= per) { fin -= per; ++fc; }
+      look_up();
     }
-    __syncwarp();
-    if (off >= 0) bulk_load(ring + fslot * P::STEP + lane * BLK, a.pool + off, BLK, bar);
-    ++copies;
-    if (++fslot == ST) fslot = 0;
-    fj += FEW_WARPS; fleft -= FEW_WARPS;
-    fc += adv_c; fin += adv_in;
-    if (fin >= per) { fin -= per; ++fc; }
-    look_up();
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
   look_up();
 #pragma unroll
   for (int s = 0; s < ST; ++s) fetch();
 
   int slot = 0;
-  uint32_t phase = 0;
   int mine = w;                                   // the warp's next step, counted from the CTA's first
   const int steps = (int)(end - start);
   int pos = 0;                                    // the segment's first
@@ -285,15 +283,16 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
       m[n][0] = m[n][1] = -INFINITY; ref[n][0] = ref[n][1] = 0.f; l[n][0] = l[n][1] = 0.f;
     }
     for (; mine < pos + seg; mine += FEW_WARPS) {
-      const bool ok = __all_sync(~0u, mbar_wait(&bars[w][slot], phase, (volatile int*)&gave_up, nullptr, a.limit));
-      const int here = present[w][slot];
+      asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+      __syncwarp();
+      const int here = present >> (4 * slot) & 0xFu;
       const unsigned char* blk = ring + slot * P::STEP;
       float s[FEW_BLOCKS][NT][4];
 #pragma unroll
       for (int k = 0; k < FEW_BLOCKS; ++k) score_block<Dh, NT, F32>(blk + k * BLK, q, s[k], g, t);
       // ---- weights
       const int tok0 = (j0 + mine - pos) * FEW_TOKENS;
-      const bool masked = tok0 > u.seq - FEW_TOKENS || here != (1 << FEW_BLOCKS) - 1 || !ok;
+      const bool masked = tok0 > u.seq - FEW_TOKENS || here != (1 << FEW_BLOCKS) - 1;
       uint32_t ph[FEW_BLOCKS][NT][2], pl[FEW_BLOCKS][F32 ? NT : 1][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -305,7 +304,6 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
               const int rel = tok0 + k * CACHE_BLOCK + g + 8 * (c >> 1) - u.seq, idx = first + 8 * n + 2 * t + (c & 1);
               const bool sees = ((here >> k) & 1) && (rel < 0 || row_sees(a, u.b, tree_row(a, idx), rel, u.rows));
               if (!sees) s[k][n][c] = -INFINITY;
-              if (!ok) s[k][n][c] = NAN;
             }
         }
         // The reference of the exponents moves only when a score passes it by more than ROOM: weights stay below
@@ -349,8 +347,8 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 #pragma unroll
       for (int k = 0; k < FEW_BLOCKS; ++k) value_block<Dh, NT, F32>(blk + k * BLK, ph[k], pl[k], o, g, t);
       __syncwarp();   // every lane has read the slot that the next copies go to
-      if (++slot == ST) { slot = 0; phase ^= 1u; }
-      if (ok) fetch();   // (a slot whose copies have not come is not used again)
+      if (++slot == ST) slot = 0;
+      fetch();
     }
     // ---- the four warps' parts of the unit
 #pragma unroll
@@ -392,12 +390,6 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
     pos += seg;
     if (pos < steps) next_unit<FewShape<NT>>(a, u);
   }
-  // after a wait that gave up copies may still be on their way into this CTA's memory
-  if (gave_up)
-    for (int s = 0; s < ST; ++s) {
-      const int n = (copies + ST - 1 - s) / ST;   // steps that went to the slot
-      for (uint32_t i = 0; n > 0 && i < a.limit && !mbar_try_wait(&bars[w][s], (n - 1) & 1); ++i) __nanosleep(100);
-    }
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -28,7 +28,7 @@ struct AttnArgs {
   int grid;                // CTAs at most
   int min_steps;           // steps that make a piece worth a CTA of its own
   unsigned limit;          // polls before a wait gives up
-  unsigned lost;           // bytes that the kernels' waits for copies expect and that do not come (0 but in the library's own tests)
+  unsigned lost;           // bytes that the waits for copies expect and that do not come (0 but in the library's own tests)
 };
 
 // pieces first..last of a unit; first < 0: nothing begins here that is to be joined

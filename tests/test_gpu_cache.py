@@ -538,8 +538,9 @@ def test_calls_on_two_streams_with_workspaces_of_their_own():
 
 @pytest.mark.parametrize("dtype,N,Hq", [(BF16, 2, 2), (F32, 7, 4), (BF16, 21, 4)])
 def test_a_wait_that_runs_out_gives_nan_and_returns(dtype, N, Hq):
-    """Copies that a kernel waits for and that never count as arrived: it gives up after a few thousand polls and its rows are NaN
-    (few rows and many, units of one CTA and cut ones); the context is usable afterwards, and shortened waits alone change nothing."""
+    """Copies that the tensor-core kernel waits for and that never count as arrived: it gives up after a few thousand polls and its rows
+    are NaN (units of one CTA and cut ones); the context is usable afterwards, and shortened waits alone change nothing.  The
+    kernels for few rows have no such waits."""
     ts = context(Nmax=N, B=4, dtype=dtype)
     lay = CacheLayout(Hq, 2, 128, 16, 300, 200, dtype)
     pool = random_pool(2, lay.pool_shape())
@@ -550,8 +551,11 @@ def test_a_wait_that_runs_out_gives_nan_and_returns(dtype, N, Hq):
     ts.set_test_mode(binding.TEST_SHORT_WAITS | binding.TEST_LOST_ARRIVAL)
     lse = torch.zeros(2, N + 1, Hq, device="cuda")
     lost = ts.tree_attention(*args, n_nodes=n, lse=lse)
-    assert torch.isnan(lost[0]).all() and torch.isnan(lost[1, 0]).all() and not lost[1, 1:].any()
-    assert torch.isnan(lse[0]).all() and torch.isnan(lse[1, 0]).all()
+    if dtype == BF16 and (N + 1) * Hq // 2 > 16:
+        assert torch.isnan(lost[0]).all() and torch.isnan(lost[1, 0]).all() and not lost[1, 1:].any()
+        assert torch.isnan(lse[0]).all() and torch.isnan(lse[1, 0]).all()
+    else:
+        assert torch.equal(lost, good)
     ts.set_test_mode(binding.TEST_SHORT_WAITS)
     assert torch.equal(ts.tree_attention(*args, n_nodes=n), good)
     ts.set_test_mode(0)
