@@ -14,7 +14,7 @@ constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
 constexpr int FEW_BLOCKS = 3;                        // blocks a warp takes in a step: what a step costs besides them is shared, their chains run side by side
 constexpr int FEW_TOKENS = FEW_BLOCKS * CACHE_BLOCK;
-template <int NT> using FewShape = AttnShape<8 * NT, FEW_TOKENS, 1, 1>;
+template <int NT> using FewShape = AttnShape<8 * NT, FEW_TOKENS, 1, 1, 8>;
 
 template <int Dh, int NT>
 struct FewPlan {
@@ -214,15 +214,18 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
   pdl_wait();
   pdl_launch_dependents();
   AttnUnit u;
-  long long start, end;
-  if (!attn_locate<FewShape<NT>, FEW_THREADS>(a, u, start, end)) return;
+  int first_step;
+  long long steps_;
+  if (!attn_locate<FewShape<NT>, FEW_THREADS>(a, u, first_step, steps_)) return;
+  const int steps = (int)steps_;
 
-  // The copies run ahead of the arithmetic, across units (each warp has a ring and copy groups of its own, nothing waits for another warp): the warp's steps are w, w + 4, .. of the CTA's piece.  The cursor
-  // stands at step fj of unit fu, in column fc and block fin of that page; the table's entries are read a step ahead.
+  // The copies run ahead of the arithmetic, across units (each warp has a ring and copy groups of its own): the warp's steps are
+  // w, w + 4, .. of the CTA's.  The cursor stands at step fj of unit fu, in column fc and block fin of that page; the table's
+  // entries are read a step ahead.
   unsigned char* ring = smem + w * ST * P::STEP;
   const int per = a.d.ps / CACHE_BLOCK, adv = FEW_WARPS * FEW_BLOCKS, adv_c = adv / per, adv_in = adv - adv_c * per;
   AttnUnit fu = u;
-  int fj = (int)(start - u.t0) + w, fleft = (int)(end - start) - w, fc = fj * FEW_BLOCKS / per, fin = fj * FEW_BLOCKS - fc * per, fh = fu.v / fu.nq;
+  int fj = first_step + w, fleft = steps - w, fc = fj * FEW_BLOCKS / per, fin = fj * FEW_BLOCKS - fc * per, fh = fu.v / fu.nq;
   int fslot = 0, page = -1, inner = 0;   // (the first lanes: a block each)
   uint32_t present = 0;                  // four bits a slot: its blocks that have a page
   auto look_up = [&]() {
@@ -265,11 +268,10 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 
   int slot = 0;
   int mine = w;                                   // the warp's next step, counted from the CTA's first
-  const int steps = (int)(end - start);
   int pos = 0;                                    // the segment's first
   while (pos < steps) {
     const int h = u.v / u.nq, first = (u.v - h * u.nq) * QT;
-    const int j0 = (int)(start + pos - u.t0);     // step of the unit at which the segment begins
+    const int j0 = pos == 0 ? first_step : 0;     // step of the unit at which the segment begins
     const int seg = min(u.n - j0, steps - pos);
     Queries<Dh, NT, F32> q;
     q.load(a, u, h, first, lane);
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
       }
     __syncthreads();
     const bool whole = seg == u.n;
-    const size_t piece = ((size_t)blockIdx.x * 2 + (start > u.t0 ? 0 : 1)) * QT;
+    const size_t piece = ((size_t)blockIdx.x * 2 + (j0 > 0 ? 0 : 1)) * QT;
     for (int e = threadIdx.x; e < QT * Dh; e += FEW_THREADS) {
       const int row = e / Dh, ch = e - row * Dh, idx = first + row;
       if (idx >= u.rows * a.d.G) continue;

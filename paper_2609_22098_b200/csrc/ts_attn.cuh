@@ -1,10 +1,11 @@
 // What the attention kernels over the 4-bit cache share: how the work is cut, who sees what, how pieces are joined.
 //
 // The work is a line of steps (a few blocks of one head for one tile of query rows): requests, then kv heads, then tiles of
-// rows, then steps.  A unit = the steps of one (request, head, tile).  A step is as long as its cost, and the line is cut
-// into equal pieces, one a CTA, whatever the lengths of the contexts are (they are known on the device only); a step belongs
-// to the piece in which it begins.  A unit that lies within one CTA is written by it; the pieces of another go to the
-// workspace, with a record by which the join kernel finds them.
+// rows, then steps.  A unit = the steps of one (request, head, tile), behind a lead that stands for what a unit costs besides
+// (queries, results).  Steps and leads are as long as their cost, and the line is cut into equal pieces, one a CTA, whatever
+// the lengths of the contexts are (they are known on the device only); a step belongs to the piece in which it begins.  A
+// unit that lies within one CTA is written by it; the pieces of another go to the workspace, with a record by which the join
+// kernel finds them.
 #pragma once
 
 #include "ts_cache.cuh"
@@ -34,13 +35,15 @@ struct AttnArgs {
 // pieces first..last of a unit; first < 0: nothing begins here that is to be joined
 struct AttnRecord { int b, v, first, last, nq; };
 
-// v = head * nq + tile; n steps of length wt each, the first at place t0; wl: the length where a head's last tile is half full
+// v = head * nq + tile; n steps of length wt each behind the lead, which begins at place t0; wl: wt where a head's last tile is
+// half full
 struct AttnUnit { int b, v, n, nq, rows, seq, wt, wl; long long t0; };
 
-// QT query rows a tile, TOK tokens a step; a step is WIDE long, HALF where at most half of the tile's rows are there
-template <int QT_, int TOK_, int WIDE_, int HALF_>
+// QT query rows a tile, TOK tokens a step; a step is WIDE long, HALF where at most half of the tile's rows are there; a lead is
+// as long as LEAD steps
+template <int QT_, int TOK_, int WIDE_, int HALF_, int LEAD_>
 struct AttnShape {
-  static constexpr int QT = QT_, TOK = TOK_, WIDE = WIDE_, HALF = HALF_;
+  static constexpr int QT = QT_, TOK = TOK_, WIDE = WIDE_, HALF = HALF_, LEAD = LEAD_;
 };
 
 // the request's units: fills all of u but v, wt and t0; returns their length together
@@ -53,7 +56,7 @@ __device__ __forceinline__ long long unit_set(const AttnArgs& a, int b, AttnUnit
   u.n = (int)max(1ll, (end + S::TOK - 1) / S::TOK);
   u.nq = (u.rows * a.d.G + S::QT - 1) / S::QT;
   u.wl = u.rows * a.d.G - (u.nq - 1) * S::QT <= S::QT / 2 ? S::HALF : S::WIDE;
-  return (long long)a.d.Hkv * u.n * ((u.nq - 1) * S::WIDE + u.wl);
+  return (long long)a.d.Hkv * (u.n + S::LEAD) * ((u.nq - 1) * S::WIDE + u.wl);
 }
 template <class S>
 __device__ __forceinline__ int unit_weight(const AttnUnit& u) { return S::WIDE == S::HALF ? S::WIDE : (u.v + 1) % u.nq == 0 ? u.wl : S::WIDE; }
@@ -67,9 +70,10 @@ __device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) {
 __device__ __forceinline__ long long piece_start(long long total, int active, int c) { return divide(total * c, active); }
 __device__ __forceinline__ int piece_of(long long total, int active, long long x) { return (int)divide((x + 1) * active + total - 1, total) - 1; }
 
+// (to be called where there is one)
 template <class S>
 __device__ __forceinline__ void next_unit(const AttnArgs& a, AttnUnit& u) {
-  u.t0 += (long long)u.n * u.wt;
+  u.t0 += (long long)(u.n + S::LEAD) * u.wt;
   if (++u.v >= a.d.Hkv * u.nq) {
     u.v = 0;
     for (int b = u.b + 1; b < a.B; ++b)
@@ -78,65 +82,75 @@ __device__ __forceinline__ void next_unit(const AttnArgs& a, AttnUnit& u) {
   u.wt = unit_weight<S>(u);
 }
 
-// Finds the unit in which this CTA's first step lies, the place of that step and the end of the piece.  All threads call it;
-// false: no step.
+// Finds this CTA's steps: the unit of the first, its number there, and how many there are.  All threads call it; false: none.
 template <class S, int THREADS>
-__device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, long long& start, long long& end) {
-  __shared__ long long wsum[THREADS / 32];
+__device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, int& first, long long& steps) {
+  __shared__ long long wsum[THREADS / 32][2], before[2];   // before: steps before the piece's beginning and end
   __shared__ AttnUnit found;
-  const int per = (a.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  AttnUnit n;
-  long long sum = 0;
-  for (int b = b0; b < min(b0 + per, a.B); ++b) sum += unit_set<S>(a, b, n);
-  long long inc = sum;
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(~0u, inc, o);
-    if (lane >= o) inc += v;
+  __shared__ int found_step;
+  const int per = (a.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long sum = 0, cnt = 0;   // length and steps of this thread's requests
+  for (int b = b0; b < b1; ++b) {
+    sum += unit_set<S>(a, b, u);
+    cnt += (long long)a.d.Hkv * u.nq * u.n;
   }
-  if (lane == 31) wsum[warp] = inc;
+  long long at = sum, nth = cnt;
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(~0u, at, o), y = __shfl_up_sync(~0u, nth, o);
+    if (lane >= o) { at += x; nth += y; }
+  }
+  if (lane == 31) { wsum[warp][0] = at; wsum[warp][1] = nth; }
+  at -= sum; nth -= cnt;
   __syncthreads();
-  long long before = 0, total = 0;
+  long long total = 0, all = 0;
   for (int w = 0; w < THREADS / 32; ++w) {
-    if (w < warp) before += wsum[w];
-    total += wsum[w];
+    if (w < warp) { at += wsum[w][0]; nth += wsum[w][1]; }
+    total += wsum[w][0]; all += wsum[w][1];
   }
   const int active = attn_active<S>(a, total);
   if (total == 0 || (int)blockIdx.x >= active) {
     if (threadIdx.x == 0) a.records[blockIdx.x].first = -1;
     return false;
   }
-  const long long x0 = piece_start(total, active, blockIdx.x);
-  end = piece_start(total, active, blockIdx.x + 1);
-  long long at = before + inc - sum;
-  if (x0 >= at && x0 < at + sum)
+  const long long x0 = piece_start(total, active, blockIdx.x), x1 = piece_start(total, active, blockIdx.x + 1);
+  if (threadIdx.x == 0 && x1 == total) before[1] = all;
+#pragma unroll 1
+  for (int side = 0; side < 2; ++side) {
+    long long x = (side ? x1 : x0) - at, k = nth;
+    if (x < 0 || x >= sum) continue;
     for (int b = b0;; ++b) {
-      const long long w = unit_set<S>(a, b, n);
-      if (x0 < at + w) {
-        const long long head = divide(w, a.d.Hkv), x = x0 - at, h = divide(x, head), q = min(divide(x - h * head, (long long)n.n * S::WIDE), (long long)n.nq - 1);
-        n.v = (int)(h * n.nq + q);
-        n.t0 = at + h * head + q * n.n * S::WIDE;
-        n.wt = unit_weight<S>(n);
-        found = n;
+      const long long w = unit_set<S>(a, b, u);
+      if (x < w) {
+        const long long len = u.n + S::LEAD, head = divide(w, a.d.Hkv), h = divide(x, head), q = min(divide(x - h * head, len * S::WIDE), (long long)u.nq - 1);
+        u.v = (int)(h * u.nq + q);
+        u.wt = unit_weight<S>(u);
+        x -= h * head + q * len * S::WIDE;   // within the unit
+        u.t0 = (side ? x1 : x0) - x;
+        const int j = (int)min(max(divide(x + u.wt - 1, u.wt) - S::LEAD, 0ll), (long long)u.n);   // the first step that begins there or later
+        before[side] = k + (long long)u.v * u.n + j;
+        if (side == 0) { found = u; found_step = j; }
         break;
       }
-      at += w;
+      x -= w;
+      k += (long long)a.d.Hkv * u.nq * u.n;
     }
+  }
   __syncthreads();
   u = found;
-  long long j = divide(x0 - u.t0 + u.wt - 1, u.wt);
-  if (j >= u.n && u.t0 + (long long)u.n * u.wt < total) { next_unit<S>(a, u); j = 0; }
-  start = u.t0 + j * u.wt;
-  const bool any = j < u.n && start < end;
+  first = found_step;
+  steps = before[1] - before[0];
+  if (first == u.n && steps > 0) { next_unit<S>(a, u); first = 0; }
   if (threadIdx.x == 0) {
-    // the first cut within the unit: the piece before this one holds its beginning
+    // the first cut between steps of the unit: the piece before this one holds its beginning
     AttnRecord r{u.b, u.v, -1, 0, u.nq};
-    if (any && j > 0 && piece_of(total, active, u.t0) == (int)blockIdx.x - 1) {
+    const long long step0 = u.t0 + (long long)S::LEAD * u.wt;
+    if (steps > 0 && first > 0 && piece_of(total, active, step0) == (int)blockIdx.x - 1) {
       r.first = blockIdx.x - 1;
-      r.last = piece_of(total, active, u.t0 + (long long)(u.n - 1) * u.wt);
+      r.last = piece_of(total, active, step0 + (long long)(u.n - 1) * u.wt);
     }
     a.records[blockIdx.x] = r;
   }
-  return any;
+  return steps > 0;
 }
 
 // Whether tree row i of request b sees the token at place rel behind the prefix (rel >= 0).

@@ -19,7 +19,7 @@ namespace ts {
 constexpr int MANY_TOKENS = 128;                  // a step
 constexpr int MANY_QT = 256;
 // A step with one tile of rows costs two thirds of one with two (1.5 us and 2.2 us in units of 16,000 tokens).
-using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 3, 2>;
+using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 3, 2, 4>;
 constexpr int MANY_SOFT = 16, MANY_CONV = 4;      // warps (converters: half for K, half for V)
 constexpr int MANY_CT = MANY_CONV / 2 * 32;       // threads of either kind
 constexpr int MANY_ISSUE = MANY_SOFT + MANY_CONV, MANY_LOAD = MANY_ISSUE + 1, MANY_WARPS = MANY_LOAD + 1;
@@ -80,8 +80,8 @@ __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"n"(MANY_SOFT * 32) : "memory"); }
 __device__ __forceinline__ void pair_sync(int quad) { asm volatile("bar.sync %0, 64;" ::"r"(2 + quad) : "memory"); }
 
-// where a CTA's piece begins and ends
-struct ManyPiece { AttnUnit u; long long start, end; };
+// a CTA's piece: its first unit, the number of its first step there, its steps
+struct ManyPiece { AttnUnit u; long long steps; int first, spare; };
 
 struct ManyShared {
   ManyPiece piece;
@@ -106,30 +106,17 @@ __device__ __forceinline__ ManyPiece my_piece(const ManyShared& sh) {
   return p;
 }
 
-// The steps of a CTA's piece that belong to one unit.
-struct ManySegment { int h, first, j0, n, two; bool whole; long long next; };
-__device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const AttnUnit& u, long long at, long long end) {
+// The steps of a CTA's piece that belong to one unit: n from j0 on; `left` steps of the piece are to be taken.
+struct ManySegment { int h, first, j0, n, two; bool whole; };
+__device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const AttnUnit& u, int j0, long long left) {
   ManySegment s;
   s.h = u.v / u.nq;
   s.first = (u.v - s.h * u.nq) * MANY_QT;
-  s.j0 = (int)(at - u.t0) / u.wt;   // (a unit has less than 2^24 steps)
-  s.n = min(u.n - s.j0, (int)(min(end - at, 1ll << 30) + u.wt - 1) / u.wt);
-  s.next = at + (long long)s.n * u.wt;
+  s.j0 = j0;
+  s.n = (int)min((long long)(u.n - j0), left);
   s.two = u.rows * a.d.G - s.first > 128;
   s.whole = s.n == u.n;
   return s;
-}
-
-// The steps of a CTA's piece, unit by unit.
-__device__ __forceinline__ int many_steps(const AttnArgs& a, AttnUnit u, long long at, long long end) {
-  int n = 0;
-  while (at < end) {
-    const ManySegment s = many_segment(a, u, at, end);
-    n += s.n;
-    at = s.next;
-    if (at < end) next_unit<ManyShape>(a, u);
-  }
-  return n;
 }
 
 // ---- loader -------------------------------------------------------------------------------------------------------------
@@ -141,10 +128,9 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
   using P = ManyPlan<Dh>;
   const ManyPiece piece = my_piece(sh);
   AttnUnit u = piece.u;
-  const long long start = piece.start, end = piece.end;
   constexpr uint32_t BLK = cache_block_bytes(Dh);
-  const int lane = threadIdx.x & 31, per = a.d.ps / CACHE_BLOCK, half_steps = 2 * many_steps(a, u, start, end);
-  int j = (int)(start - u.t0) / u.wt + (lane >> 3), mine = lane >> 2;   // the lane's step within its unit, its half-step in all
+  const int lane = threadIdx.x & 31, per = a.d.ps / CACHE_BLOCK, half_steps = 2 * (int)piece.steps;
+  int j = piece.first + (lane >> 3), mine = lane >> 2;   // the lane's step within its unit, its half-step in all
   int page = -1, inner = 0;
   auto look_up = [&]() {
     page = -1;
@@ -283,15 +269,16 @@ __device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* r
   using P = ManyPlan<Dh>;
   const ManyPiece piece = my_piece(sh);
   AttnUnit u = piece.u;
-  const long long end = piece.end;
   const int lane = threadIdx.x & 31;
   volatile int* abort = (volatile int*)&sh.abort;
   int slot = 0, gj = 0;
   uint32_t phase = 0;
   uint32_t used = 0;   // who read the stages last: bits of groups, by stage
   uint32_t turn = 0;   // parity of the uses so far, a bit for each group and stage
-  for (long long at = piece.start; at < end;) {
-    const ManySegment s = many_segment(a, u, at, end);
+  long long left = piece.steps;
+  for (int j0 = piece.first; left > 0; j0 = 0) {
+    const ManySegment s = many_segment(a, u, j0, left);
+    left -= s.n;
 #pragma unroll 1
     for (int j = 0; j < s.n; ++j, ++gj) {
       const int st = gj & 1;
@@ -318,8 +305,7 @@ __device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* r
       used = (used & ~(3u << (2 * st))) | by << (2 * st);
       turn ^= by << (2 * st);
     }
-    at = s.next;
-    if (at < end) next_unit<ManyShape>(a, u);
+    if (left > 0) next_unit<ManyShape>(a, u);
   }
 }
 
@@ -332,15 +318,16 @@ __device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* sme
   using P = ManyPlan<Dh>;
   const ManyPiece piece = my_piece(sh);
   AttnUnit u = piece.u;
-  const long long end = piece.end;
   volatile int* abort = (volatile int*)&sh.abort;
   constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(MANY_TOKENS >> 3) << 17) | ((128u >> 4) << 24);              // D = f32, A = B = f16, M = 128; B K-major: keys
   constexpr uint32_t id_o = (1u << 4) | (1u << 16) | ((uint32_t)(Dh >> 3) << 17) | ((128u >> 4) << 24);          // B MN-major: values
   const uint64_t qd = smem_desc(smem_u32(smem + P::Q), 16u, 1024u), kd = smem_desc(smem_u32(smem + P::K), 16u, 1024u), vd = smem_desc(smem_u32(smem + P::V), P::SLAB, 1024u);
   uint32_t weights = 0, segments = 0;   // weights: parity of the waits for each group's
   int base = 0;                         // steps before this segment
-  for (long long at = piece.start; at < end; ++segments) {
-    const ManySegment s = many_segment(a, u, at, end);
+  long long left = piece.steps;
+  for (int j0 = piece.first; left > 0; j0 = 0, ++segments) {
+    const ManySegment s = many_segment(a, u, j0, left);
+    left -= s.n;
     const int ops = s.two ? 2 * s.n : s.n;
     // product i: group i & 1, step i / 2 (two tiles) or i; its P V is issued two products later
 #pragma unroll 1
@@ -382,8 +369,7 @@ __device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* sme
       }
     }
     base += s.n;
-    at = s.next;
-    if (at < end) next_unit<ManyShape>(a, u);
+    if (left > 0) next_unit<ManyShape>(a, u);
   }
 }
 
@@ -538,7 +524,6 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
   using P = ManyPlan<Dh>;
   const ManyPiece piece = my_piece(sh);
   AttnUnit u = piece.u;
-  const long long end = piece.end;
   volatile int* abort = (volatile int*)&sh.abort;
   // group, half of a step's tokens, row of the tile (a warp reaches the 32 rows of its number modulo 4)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, grp = warp >> 3, hh = (warp >> 2) & 1, quad = warp & 3, row = quad * 32 + lane;
@@ -548,8 +533,10 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
   uint32_t count = 0;   // products of this group
   int base = 0;
   bool alive = true, apart = false;   // apart: the groups had tiles of their own in the unit before
-  for (long long at = piece.start; at < end;) {
-    const ManySegment s = many_segment(a, u, at, end);
+  long long left = piece.steps;
+  for (int j0 = piece.first; left > 0; j0 = 0) {
+    const ManySegment s = many_segment(a, u, j0, left);
+    left -= s.n;
     const int idx = s.first + (s.two ? grp * 128 : 0) + row, i = tree_row(a, idx);
     // The warps of 32 rows load a share each, of their own tile or of the shared one, which the first group's products of the
     // unit before may still read.
@@ -639,7 +626,7 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
     if (!alive || *abort) sum = NAN;
     tc_fence_after();
     const int rows = u.rows * a.d.G;
-    const size_t slot = ((size_t)blockIdx.x * 2 + (piece.start > u.t0 ? 0 : 1)) * MANY_QT + (s.two ? grp * 128 : 0) + row;
+    const size_t slot = ((size_t)blockIdx.x * 2 + (s.j0 > 0 ? 0 : 1)) * MANY_QT + (s.two ? grp * 128 : 0) + row;
     const float inv = s.whole ? row_inv(sum) * a.vo : 1.f;
     const int n = s.two ? Dh / 64 : 1, c_lo = (s.two ? hh : grp * 2 + hh) * n, c_hi = min(c_lo + n, Dh / 32);   // groups of 32 channels
 #pragma unroll 1
@@ -701,8 +688,7 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
     if (s.two) pair_sync(grp * 4 + quad);
     else soft_sync();
     base += s.n;
-    at = s.next;
-    if (at < end) next_unit<ManyShape>(a, u);
+    if (left > 0) next_unit<ManyShape>(a, u);
   }
 }
 
@@ -727,13 +713,14 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
   pdl_wait();
   pdl_launch_dependents();
   AttnUnit u;
-  long long start, end;
-  if (!attn_locate<ManyShape, MANY_THREADS>(a, u, start, end)) return;
+  int first;
+  long long steps;
+  if (!attn_locate<ManyShape, MANY_THREADS>(a, u, first, steps)) return;
   if (warp == MANY_ISSUE) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (threadIdx.x == 0) { sh.piece.u = u; sh.piece.start = start; sh.piece.end = end; }
+  if (threadIdx.x == 0) { sh.piece.u = u; sh.piece.first = first; sh.piece.steps = steps; }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
