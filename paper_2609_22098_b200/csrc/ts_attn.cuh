@@ -2,10 +2,9 @@
 //
 // The work is a line of steps (a few blocks of one head for one tile of query rows): requests, then kv heads, then tiles of
 // rows, then steps.  A unit = the steps of one (request, head, tile), behind a lead that stands for what a unit costs besides
-// (queries, results).  Steps and leads are as long as their cost, and the line is cut into equal pieces, one a CTA, whatever
-// the lengths of the contexts are (they are known on the device only); a step belongs to the piece in which it begins.  A
-// unit that lies within one CTA is written by it; the pieces of another go to the workspace, with a record by which the join
-// kernel finds them.
+// (queries, results).  The line is cut into equal pieces, one a CTA, whatever the lengths of the contexts are (they are known on the
+// device only).  A unit that lies within one CTA is written by it; the pieces of another go to the workspace, with a record by
+// which the join kernel finds them.
 #pragma once
 
 #include "ts_cache.cuh"
@@ -35,51 +34,44 @@ struct AttnArgs {
 // pieces first..last of a unit; first < 0: nothing begins here that is to be joined
 struct AttnRecord { int b, v, first, last, nq; };
 
-// v = head * nq + tile; n steps of length wt each behind the lead, which begins at place t0; wl: wt where a head's last tile is
-// half full
-struct AttnUnit { int b, v, n, nq, rows, seq, wt, wl; long long t0; };
+// v = head * nq + tile; n steps behind the lead, which begins at place t0
+struct AttnUnit { int b, v, n, nq, rows, seq; long long t0; };
 
-// QT query rows a tile, TOK tokens a step; a step is WIDE long, HALF where at most half of the tile's rows are there; a lead is
-// as long as LEAD steps
-template <int QT_, int TOK_, int WIDE_, int HALF_, int LEAD_>
+// QT query rows a tile, TOK tokens a step; a lead is as long as LEAD steps
+template <int QT_, int TOK_, int LEAD_>
 struct AttnShape {
-  static constexpr int QT = QT_, TOK = TOK_, WIDE = WIDE_, HALF = HALF_, LEAD = LEAD_;
+  static constexpr int QT = QT_, TOK = TOK_, LEAD = LEAD_;
 };
 
-// the request's units: fills all of u but v, wt and t0; returns their length together
+// the request's units: fills all of u but v and t0; returns how many there are
 template <class S>
-__device__ __forceinline__ long long unit_set(const AttnArgs& a, int b, AttnUnit& u) {
+__device__ __forceinline__ int unit_set(const AttnArgs& a, int b, AttnUnit& u) {
   u.b = b; u.seq = a.seq_len[b];
   u.rows = request_rows(a.n_nodes, b, a.rcap);
-  if (u.seq < 0) { u.n = 0; u.nq = 0; u.wl = 0; return 0; }
+  if (u.seq < 0) { u.n = 0; u.nq = 0; return 0; }
   const long long end = min((long long)u.seq + u.rows, (long long)a.d.cols * a.d.ps);   // (no page beyond the table's)
   u.n = (int)max(1ll, (end + S::TOK - 1) / S::TOK);
   u.nq = (u.rows * a.d.G + S::QT - 1) / S::QT;
-  u.wl = u.rows * a.d.G - (u.nq - 1) * S::QT <= S::QT / 2 ? S::HALF : S::WIDE;
-  return (long long)a.d.Hkv * (u.n + S::LEAD) * ((u.nq - 1) * S::WIDE + u.wl);
+  return a.d.Hkv * u.nq;
 }
-template <class S>
-__device__ __forceinline__ int unit_weight(const AttnUnit& u) { return S::WIDE == S::HALF ? S::WIDE : (u.v + 1) % u.nq == 0 ? u.wl : S::WIDE; }
 
 // (a division of 64 bits is a call of a hundred instructions; almost all of these fit 32)
 __device__ __forceinline__ long long divide(long long x, long long y) { return (unsigned long long)(x | y) >> 32 ? x / y : (long long)((unsigned)x / (unsigned)y); }
 
 // CTAs that take part, where piece c begins, and the piece in which place x lies
-template <class S>
-__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, divide(total, a.min_steps * S::WIDE))); }
+__device__ __forceinline__ int attn_active(const AttnArgs& a, long long total) { return (int)min((long long)a.grid, max(1ll, divide(total, a.min_steps))); }
 __device__ __forceinline__ long long piece_start(long long total, int active, int c) { return divide(total * c, active); }
 __device__ __forceinline__ int piece_of(long long total, int active, long long x) { return (int)divide((x + 1) * active + total - 1, total) - 1; }
 
 // (to be called where there is one)
 template <class S>
 __device__ __forceinline__ void next_unit(const AttnArgs& a, AttnUnit& u) {
-  u.t0 += (long long)(u.n + S::LEAD) * u.wt;
+  u.t0 += u.n + S::LEAD;
   if (++u.v >= a.d.Hkv * u.nq) {
     u.v = 0;
     for (int b = u.b + 1; b < a.B; ++b)
       if (unit_set<S>(a, b, u) > 0) break;
   }
-  u.wt = unit_weight<S>(u);
 }
 
 // Finds this CTA's steps: the unit of the first, its number there, and how many there are.  All threads call it; false: none.
@@ -91,8 +83,9 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, int& first, long lon
   const int per = (a.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long sum = 0, cnt = 0;   // length and steps of this thread's requests
   for (int b = b0; b < b1; ++b) {
-    sum += unit_set<S>(a, b, u);
-    cnt += (long long)a.d.Hkv * u.nq * u.n;
+    const long long units = unit_set<S>(a, b, u);
+    sum += units * (u.n + S::LEAD);
+    cnt += units * u.n;
   }
   long long at = sum, nth = cnt;
   for (int o = 1; o < 32; o <<= 1) {
@@ -107,7 +100,7 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, int& first, long lon
     if (w < warp) { at += wsum[w][0]; nth += wsum[w][1]; }
     total += wsum[w][0]; all += wsum[w][1];
   }
-  const int active = attn_active<S>(a, total);
+  const int active = attn_active(a, total);
   if (total == 0 || (int)blockIdx.x >= active) {
     if (threadIdx.x == 0) a.records[blockIdx.x].first = -1;
     return false;
@@ -119,34 +112,31 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, int& first, long lon
     long long x = (side ? x1 : x0) - at, k = nth;
     if (x < 0 || x >= sum) continue;
     for (int b = b0;; ++b) {
-      const long long w = unit_set<S>(a, b, u);
-      if (x < w) {
-        const long long len = u.n + S::LEAD, head = divide(w, a.d.Hkv), h = divide(x, head), q = min(divide(x - h * head, len * S::WIDE), (long long)u.nq - 1);
-        u.v = (int)(h * u.nq + q);
-        u.wt = unit_weight<S>(u);
-        x -= h * head + q * len * S::WIDE;   // within the unit
+      const long long units = unit_set<S>(a, b, u), len = u.n + S::LEAD;
+      if (x < units * len) {
+        u.v = (int)divide(x, len);
+        x -= u.v * len;   // within the unit
         u.t0 = (side ? x1 : x0) - x;
-        const int j = (int)min(max(divide(x + u.wt - 1, u.wt) - S::LEAD, 0ll), (long long)u.n);   // the first step that begins there or later
+        const int j = (int)max(x - S::LEAD, 0ll);   // the first step that begins there or later
         before[side] = k + (long long)u.v * u.n + j;
         if (side == 0) { found = u; found_step = j; }
         break;
       }
-      x -= w;
-      k += (long long)a.d.Hkv * u.nq * u.n;
+      x -= units * len;
+      k += units * u.n;
     }
   }
   __syncthreads();
   u = found;
   first = found_step;
   steps = before[1] - before[0];
-  if (first == u.n && steps > 0) { next_unit<S>(a, u); first = 0; }
   if (threadIdx.x == 0) {
     // the first cut between steps of the unit: the piece before this one holds its beginning
     AttnRecord r{u.b, u.v, -1, 0, u.nq};
-    const long long step0 = u.t0 + (long long)S::LEAD * u.wt;
+    const long long step0 = u.t0 + S::LEAD;
     if (steps > 0 && first > 0 && piece_of(total, active, step0) == (int)blockIdx.x - 1) {
       r.first = blockIdx.x - 1;
-      r.last = piece_of(total, active, step0 + (long long)(u.n - 1) * u.wt);
+      r.last = piece_of(total, active, step0 + u.n - 1);
     }
     a.records[blockIdx.x] = r;
   }

@@ -18,8 +18,10 @@ namespace ts {
 
 constexpr int MANY_TOKENS = 128;                  // a step
 constexpr int MANY_QT = 256;
-// A step with one tile of rows costs two thirds of one with two (1.5 us and 2.2 us in units of 16,000 tokens).
-using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 3, 2, 4>;
+// A lead of four steps (trees of 32 requests behind 500 to 6,000 tokens, us, with leads of 0, 2, 4, 6, 9: 161, 135, 122, 125, 128).  Steps
+// with one and with two tiles count alike: 1.5 and 2.2 us, but what they wait for is the same (counted as 2 to 3: 298 us for
+// 281 where both occur).
+using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 4>;
 constexpr int MANY_SOFT = 16, MANY_CONV = 4;      // warps (converters: half for K, half for V)
 constexpr int MANY_CT = MANY_CONV / 2 * 32;       // threads of either kind
 constexpr int MANY_ISSUE = MANY_SOFT + MANY_CONV, MANY_LOAD = MANY_ISSUE + 1, MANY_WARPS = MANY_LOAD + 1;
