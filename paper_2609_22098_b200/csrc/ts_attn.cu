@@ -8,11 +8,15 @@ namespace ts {
 // ------------------------------------------------------------------------------------------------
 // Few rows: 8 NT query rows of one kv head a unit, on mma.sync with the cache's tokens on the rows of the matrix
 // instruction (S^T = K Q^T, O^T = V^T P^T), so that one instruction of 16 x 8 serves eight query rows and no lane computes
-// for rows that are not there.
+// for rows that are not there.  Single tokens of 64 requests of 1,000 to 16,000 tokens with eight kv heads of 128 channels (626 MB of
+// cache): 169 us, 3.7 TB/s.  The copies alone take 107 to 119 us; what is left is instruction issue, some 370 a block of 16 tokens (unpacking
+// 4,096 codes is half of them), at two a cycle of four.
 // ------------------------------------------------------------------------------------------------
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
-constexpr int FEW_BLOCKS = 3;                        // blocks a warp takes in a step: what a step costs besides them is shared, their chains run side by side
+// Blocks a warp takes in a step: what a step costs besides them is shared, and their chains run side by side.  (2, 3, 4 blocks: the
+// batch above takes 206, 184, 198 us; with four the registers leave room for two CTAs an SM.)
+constexpr int FEW_BLOCKS = 3;
 constexpr int FEW_TOKENS = FEW_BLOCKS * CACHE_BLOCK;
 // A lead of eight steps (64 requests of 1,000 to 16,000 tokens, us, with leads of 0, 2, 4, 8, 12, 16: 184, 185, 179, 170, 173, 176).
 template <int NT> using FewShape = AttnShape<8 * NT, FEW_TOKENS, 8>;
@@ -397,70 +401,95 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 
 // ------------------------------------------------------------------------------------------------
 // Join: a CTA takes some rows of a cut unit, a warp a row; where there are many pieces, all its warps one row after the
-// other.  The pieces are added in an order that depends on their number only.
+// other.  The pieces are added in an order that depends on their number only.  Bound by latency (the record, then sums and
+// pieces, which are loaded together): 2 us of 10 for one request of 517 tokens, 7 of 114 for 32 trees, 13 of 274 for 8
+// requests with trees of 120 to 256 nodes (up to 38 MB of pieces, from L2).
 // ------------------------------------------------------------------------------------------------
 constexpr int JOIN_WARPS = 8;
+// Rows a CTA: few rows are cut into many pieces, which a CTA's warps share (1, 2, 4, 8 rows: the request 12.1, 10.3, 10.0, 10.0 us, two
+// contexts of 130,000 tokens 58, 57, 58, 61, four of up to 3,000 13.9, 13.2, 14.9, 14.9); of many rows fewer mean more CTAs
+// that find nothing (8, 16, 32 rows: the 32 trees 117, 114, 116 us).
+constexpr int JOIN_FEW = 2, JOIN_MANY = 16;
+constexpr int JOIN_BATCH = 4;   // pieces whose loads a warp has in flight (8: the trees 121 us for 117)
 
 template <int Dh, typename T>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) attn_join_kernel(const AttnArgs a, int QT, int per) {
-  constexpr int V = Dh / 32;
-  __shared__ float acc[JOIN_WARPS][Dh], red[JOIN_WARPS][2];
+  constexpr int V = Dh / 32;   // channels of a lane
+  using Vec = typename std::conditional<V == 4, float4, float2>::type;
+  __shared__ float acc[JOIN_WARPS][Dh], red[JOIN_WARPS];
   pdl_wait();
   pdl_launch_dependents();
   const AttnRecord r = a.records[blockIdx.x];
   if (r.first < 0) return;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, n = r.last - r.first + 1;
   const int h = r.v / r.nq, first = (r.v - h * r.nq) * QT, r0 = blockIdx.y * per;
-  const int rows = min(min(QT, r0 + per), request_rows(a.n_nodes, r.b, a.rcap) * a.d.G - first);   // of the tile, that are there
-  const int rw = n > 2 * JOIN_WARPS ? JOIN_WARPS : 1, part = rw > 1 ? w : 0;                             // warps a row
+  const int rows = min(min(QT, r0 + per), r.rows * a.d.G - first);        // of the tile, that are there
+  const int rw = n > 2 * JOIN_WARPS ? JOIN_WARPS : 1, part = rw > 1 ? w : 0;   // warps a row
   for (int row = r0 + (rw > 1 ? 0 : w); row < rows; row += rw > 1 ? 1 : JOIN_WARPS) {
     // piece k: the first begins at or before the unit and is its CTA's last; the others begin within it
     auto at = [&](int k) { return ((size_t)(r.first + k) * 2 + (k == 0 ? 1 : 0)) * QT + row; };
+    float2 ml[JOIN_BATCH];
+    Vec y[JOIN_BATCH];
+    auto load = [&](int k0) {
+#pragma unroll
+      for (int i = 0; i < JOIN_BATCH; ++i) {
+        const int k = k0 + i * rw;
+        ml[i] = make_float2(-INFINITY, 0.f);
+        y[i] = Vec{};
+        if (k < n) {
+          ml[i] = *reinterpret_cast<const float2*>(a.part_ml + 2 * at(k));
+          y[i] = *reinterpret_cast<const Vec*>(a.part + at(k) * Dh + lane * V);
+        }
+      }
+    };
+    load(part);   // (on their way together with what the largest reference needs)
     float top = -INFINITY;
     for (int k = lane; k < n; k += 32) top = fmaxf(top, a.part_ml[2 * at(k)]);
 #pragma unroll
     for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, x));
     float sum = 0.f, x[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = 0.f;
-#pragma unroll 4
-    for (int k = part; k < n; k += rw) {
-      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * at(k));
-      const float wgt = part_weight(ml.x, top);
-      sum += wgt * ml.y;
+    for (int v = 0; v < V; ++v) x[v] = 0.f;
+    for (int k0 = part; k0 < n;) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] += wgt * a.part[at(k) * Dh + lane + 32 * i];
+      for (int i = 0; i < JOIN_BATCH; ++i) {
+        const float wgt = part_weight(ml[i].x, top);
+        sum += wgt * ml[i].y;
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] += wgt * reinterpret_cast<const float*>(&y[i])[v];
+      }
+      k0 += JOIN_BATCH * rw;
+      if (k0 < n) load(k0);
     }
     if (rw > 1) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) acc[w][lane + 32 * i] = x[i];
-      if (lane == 0) red[w][1] = sum;
+      for (int v = 0; v < V; ++v) acc[w][lane * V + v] = x[v];
+      if (lane == 0) red[w] = sum;
       __syncthreads();
       sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = 0.f;
+      for (int v = 0; v < V; ++v) x[v] = 0.f;
 #pragma unroll
       for (int k = 0; k < JOIN_WARPS; ++k) {
-        sum += red[k][1];
+        sum += red[k];
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] += acc[k][lane + 32 * i];
+        for (int v = 0; v < V; ++v) x[v] += acc[k][lane * V + v];
       }
       __syncthreads();
       if (w > 0) continue;
     }
     const int idx = first + row;
-    T* out = reinterpret_cast<T*>(a.out) + out_row(a, r.b, h, idx);
+    T* out = reinterpret_cast<T*>(a.out) + out_row(a, r.b, h, idx) + lane * V;
     const float inv = row_inv(sum) * a.vo;
 #pragma unroll
-    for (int i = 0; i < V; ++i) store_out(out + lane + 32 * i, x[i] * inv);
+    for (int v = 0; v < V; ++v) store_out(out + v, x[v] * inv);
     if (lane == 0 && a.lse) a.lse[lse_row(a, r.b, h, idx)] = row_lse(top, sum);
   }
 }
 
 cudaError_t attn_join(ts_ctx* ctx, const AttnArgs& a, int QT, bool f32, cudaStream_t st) {
   ProfScope ps(ctx, K_ATTN_JOIN, st);
-  // rows a CTA: few rows are cut into many pieces, which a CTA's warps share; many rows would be many CTAs
-  const int per = QT > 16 ? 32 : 2;
+  const int per = QT > 16 ? JOIN_MANY : JOIN_FEW;
   void (*kernel)(const AttnArgs, int, int) = f32 ? (a.d.Dh == 128 ? attn_join_kernel<128, float> : attn_join_kernel<64, float>)
                                             : (a.d.Dh == 128 ? attn_join_kernel<128, __nv_bfloat16> : attn_join_kernel<64, __nv_bfloat16>);
   return launch_kernel(kernel, dim3(a.grid, (QT + per - 1) / per), dim3(JOIN_WARPS * 32), 0, st, true, a, QT, per);
@@ -478,7 +507,9 @@ void attn_place(AttnArgs& a, int QT, char* ws) {
   a.part_ml = (float*)((char*)a.part + round256((size_t)a.grid * 2 * QT * a.d.Dh * 4));
 }
 
-// Query rows of a unit and CTAs of a launch.
+// Query rows of a unit and CTAs of a launch.  Two tiles of eight rows share the unpacked keys and values, one tile leaves room for
+// three CTAs an SM (32 requests of 500 to 8,000 tokens, one tile and two: 9 rows 145 and 99 us, 16 rows 143 and 109; 8 rows need
+// only one).  fp32 takes one: its queries and weights are two parts each, which do not fit twice.
 static int few_tiles_of(const CacheDims& d, int rcap, bool f32) { return !f32 && (long long)rcap * d.G > 8 ? 2 : 1; }
 static int few_ctas(int nt, bool f32) { return f32 || nt > 1 ? 2 : 3; }
 
@@ -523,7 +554,8 @@ static cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, 
   return f32 ? launch_few<64, 1, true>(ctx, a, st) : nt == 2 ? launch_few<64, 2, false>(ctx, a, st) : launch_few<64, 1, false>(ctx, a, st);
 }
 
-// Which kernel: tiles of 16 rows read the keys and values again for every tile, tiles of 128 pay for rows that are not there.
+// Which kernel: tiles of 16 rows read the keys and values again for every tile, tiles of 128 pay for rows that are not there (32
+// requests of 500 to 8,000 tokens, few and many: 16 rows 109 and 150 us, 17 rows 178 and 154, 32 rows 198 and 160).
 static bool takes_many(const CacheDims& d, int rcap, bool f32) { return !f32 && (long long)rcap * d.G > 16; }
 
 }  // namespace ts
@@ -552,7 +584,7 @@ extern "C" int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* lay, in
   const bool f32 = lay->dtype == TS_DTYPE_F32;
   const int64_t unit = f32 ? 4 : 8, least = (int64_t)lay->Hq * lay->Dh;
   if (ldq < least || ldo < least || ldq % unit || ldo % unit) return set_error(TS_ERR_INVALID, "ts_tree_attention: row strides must cover Hq * Dh elements and be multiples of 16 bytes");
-  if (!(fabsf(scale) <= 1e30f)) return set_error(TS_ERR_INVALID, "ts_tree_attention: scale must be finite");
+  if (!(fabsf(scale) <= 1e30f && fabsf(ldexpf(scale, lay->k_exp)) <= 1e30f)) return set_error(TS_ERR_INVALID, "ts_tree_attention: scale (and scale * 2^k_exp) must be at most 1e30 in magnitude");
   if (ws_bytes < ts_tree_attention_workspace_bytes(ctx, lay, B)) return set_error(TS_ERR_WORKSPACE, "ts_tree_attention: workspace too small");
   if (!on_ctx_device(ctx)) return set_error(TS_ERR_INVALID, "ts_tree_attention: the context's device is not the current one");
   AttnArgs a{};

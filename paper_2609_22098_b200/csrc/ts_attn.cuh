@@ -32,7 +32,7 @@ struct AttnArgs {
 };
 
 // pieces first..last of a unit; first < 0: nothing begins here that is to be joined
-struct AttnRecord { int b, v, first, last, nq; };
+struct AttnRecord { int b, v, first, last, nq, rows; };
 
 // v = head * nq + tile; n steps behind the lead, which begins at place t0
 struct AttnUnit { int b, v, n, nq, rows, seq; long long t0; };
@@ -132,7 +132,7 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, int& first, long lon
   steps = before[1] - before[0];
   if (threadIdx.x == 0) {
     // the first cut between steps of the unit: the piece before this one holds its beginning
-    AttnRecord r{u.b, u.v, -1, 0, u.nq};
+    AttnRecord r{u.b, u.v, -1, 0, u.nq, u.rows};
     const long long step0 = u.t0 + S::LEAD;
     if (steps > 0 && first > 0 && piece_of(total, active, step0) == (int)blockIdx.x - 1) {
       r.first = blockIdx.x - 1;

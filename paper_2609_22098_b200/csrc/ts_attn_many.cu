@@ -9,6 +9,12 @@
 // A unit has up to 256 query rows.  With more than 128 the groups take a tile of 128 rows each, and both read the same
 // converted keys and values; with fewer they take the same rows and every other step, and their halves are joined at the end.
 // Either way one group's exponentials run beside the other's matrix products.
+//
+// Trees of 120 to 256 nodes of 8 requests behind 2,000 to 16,000 tokens, 32 query heads on 4 of 128 channels: 274 us, 0.71 PFLOP/s, 44 % of
+// what a large matrix product reaches.  Trees of 8 to 30 nodes of 32 requests behind 500 to 6,000 tokens, 8 kv heads: 114 us, 1.1 TB/s.  A
+// step takes 2.2 us with two tiles and 1.5 with one; its products keep the tensor cores busy for 39 % of the time and its
+// exponentials their unit for 39 %.  What bounds it is the chain of a tile (scores, their largest, weights, products) and the
+// waits between its links, which two groups cover in part; with one tile the converters (64 KB of fp16 a step) are as busy.
 #include <string.h>
 
 #include "ts_attn.cuh"

@@ -40,9 +40,11 @@ bool on_ctx_device(const ts_ctx* ctx) {
 
 // ------------------------------------------------------------------------------------------------
 // Reserve.  Every CTA adds up the pages that all requests need (a few thousand at most), then serves its share of the
-// requests, one warp each (and all of its warps for the many entries of a request that starts).  Small calls are one launch of a cluster of eight CTAs whose barrier separates reading the
-// counts from writing them, so that they may be updated in place; where whole tables are written, many CTAs write them and a
-// second launch updates the counts.
+// requests, one warp each (and all of its warps for the many entries of a request that starts).  Small calls are one launch of a
+// cluster of eight CTAs whose barrier separates reading the counts from writing them, so that they may be updated in place;
+// where whole tables are written, many CTAs write them and a second launch updates the counts.  Bound by latency (counts, a scan, entries,
+// slots and two barriers one after the other): a round of 32 requests moves 9 KB in 7.6 us, 500 requests that start with tables of
+// up to 1,875 entries move 3.8 MB in 17.6.
 // ------------------------------------------------------------------------------------------------
 constexpr int RES_THREADS = 512;
 constexpr int RES_CLUSTER = 8;
@@ -257,7 +259,9 @@ static cudaError_t launch_reserve(ts_ctx* ctx, const ReserveArgs& a, cudaStream_
 
 // ------------------------------------------------------------------------------------------------
 // Append.  A lane takes eight elements of a row's head (two lanes share a scale), Dh/4 lanes both K and V of one (row, head),
-// so that what is not finite in either marks both.
+// so that what is not finite in either marks both.  Chunks of 64 requests (102 to 257 rows each, 4 heads of 64 channels, fp32, with
+// values): 16.7 us for 50 MB, 3 TB/s; the trees of 32 requests in bf16 9 us for 11 MB.  Bound by issue and by the ramp of so
+// short a kernel; two rows a lane, side by side, took as long.
 // ------------------------------------------------------------------------------------------------
 constexpr int APP_THREADS = 256;
 
@@ -385,7 +389,9 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
 
 // ------------------------------------------------------------------------------------------------
 // Commit.  A warp per (request, layer, head) holds the bytes of all moved rows before it writes one: sources and targets of
-// a path overlap.  The CTAs of a request form a cluster, whose barrier lets the new length overwrite the old.
+// a path overlap.  The CTAs of a request form a cluster, whose barrier lets the new length overwrite the old.  Bound by latency
+// (nodes, table, bytes, then the writes): paths of up to eight rows of 32 requests, 12 layers of 8 heads, 8.5 us for 4 MB; of one
+// request with 36 layers 11 us for 0.6 MB.
 // ------------------------------------------------------------------------------------------------
 constexpr int COM_THREADS = 1024;   // at most: a warp for each layer and head of a request where 256 are enough
 constexpr int COM_CLUSTER = 8;

@@ -124,3 +124,11 @@ def test_another_device_is_refused(lib, ctx):
     assert b"device" in lib.ts_last_error_string()
     assert append(lib, ctx, layout()) == -1 and b"device" in lib.ts_last_error_string()
     assert commit(lib, ctx, layout()) == -1 and b"device" in lib.ts_last_error_string()
+
+
+def test_scales_beyond_the_range(lib, ctx):
+    """|scale| and |scale| * 2^k_exp may be 1e30 at most: their product with the queries' power of two has to be a float."""
+    for scale, k_exp in ((2e30, 0), (-2e30, -30), (1e22, 30), (-1e22, 30)):
+        assert attention(lib, ctx, layout(k_exp=k_exp), scale=scale) == -1 and b"scale" in lib.ts_last_error_string()
+    assert attention(lib, ctx, layout(k_exp=-30), scale=1e30) == -1 and b"device" in lib.ts_last_error_string()
+    assert attention(lib, ctx, layout(k_exp=30), scale=9e20) == -1 and b"device" in lib.ts_last_error_string()
