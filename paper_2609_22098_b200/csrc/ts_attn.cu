@@ -509,8 +509,9 @@ void attn_place(AttnArgs& a, int QT, char* ws) {
 
 // Query rows of a unit and CTAs of a launch.  Two tiles of eight rows share the unpacked keys and values, one tile leaves room for
 // three CTAs an SM (32 requests of 500 to 8,000 tokens, one tile and two: 9 rows 145 and 99 us, 16 rows 143 and 109; 8 rows need
-// only one).  fp32 takes one: its queries and weights are two parts each, which do not fit twice.
-static int few_tiles_of(const CacheDims& d, int rcap, bool f32) { return !f32 && (long long)rcap * d.G > 8 ? 2 : 1; }
+// only one; fp32 with 64 channels, 32 rows behind two contexts of up to 131,000 tokens 57 and 47).  fp32 with 128 channels takes
+// one: queries and weights of two parts each do not fit twice without spilling (16 requests of up to 4,000 tokens 26 and 30 us).
+static int few_tiles_of(const CacheDims& d, int rcap, bool f32) { return (long long)rcap * d.G > 8 && !(f32 && d.Dh == 128) ? 2 : 1; }
 static int few_ctas(int nt, bool f32) { return f32 || nt > 1 ? 2 : 3; }
 
 static size_t attn_few_workspace(const ts_ctx* ctx, const CacheDims& d, bool f32) {
@@ -537,7 +538,7 @@ cudaError_t attn_setup(ts_ctx* ctx) {
   cudaError_t e = cudaSuccess;
   auto allow = [&](auto kernel) { if (e == cudaSuccess) e = allow_all_smem(kernel, ctx->max_smem); };
   allow(attn_few_kernel<128, 1, false>); allow(attn_few_kernel<128, 2, false>); allow(attn_few_kernel<128, 1, true>);
-  allow(attn_few_kernel<64, 1, false>); allow(attn_few_kernel<64, 2, false>); allow(attn_few_kernel<64, 1, true>);
+  allow(attn_few_kernel<64, 1, false>); allow(attn_few_kernel<64, 2, false>); allow(attn_few_kernel<64, 1, true>); allow(attn_few_kernel<64, 2, true>);
   if (e == cudaSuccess) e = attn_many_setup(ctx);
   // the same split of L1 and shared memory as the kernels before it and after: an SM that changes it has to run empty first
   auto shared = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared); };
@@ -550,8 +551,9 @@ static cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, 
   a.grid = ctx->num_sms * few_ctas(nt, f32);
   a.min_steps = FEW_WARPS;
   attn_place(a, 8 * nt, ws);
-  if (a.d.Dh == 128) return f32 ? launch_few<128, 1, true>(ctx, a, st) : nt == 2 ? launch_few<128, 2, false>(ctx, a, st) : launch_few<128, 1, false>(ctx, a, st);
-  return f32 ? launch_few<64, 1, true>(ctx, a, st) : nt == 2 ? launch_few<64, 2, false>(ctx, a, st) : launch_few<64, 1, false>(ctx, a, st);
+  const auto launch = a.d.Dh == 128 ? f32 ? launch_few<128, 1, true> : nt == 2 ? launch_few<128, 2, false> : launch_few<128, 1, false>
+                                    : f32 ? nt == 2 ? launch_few<64, 2, true> : launch_few<64, 1, true> : nt == 2 ? launch_few<64, 2, false> : launch_few<64, 1, false>;
+  return launch(ctx, a, st);
 }
 
 // Which kernel: tiles of 16 rows read the keys and values again for every tile, tiles of 128 pay for rows that are not there (32

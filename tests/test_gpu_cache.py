@@ -351,7 +351,7 @@ def random_pool(rng_seed, shape):
 @pytest.mark.parametrize("dtype,Hq,Hkv,Dh,ps,lens,N,n_nodes", [
     (BF16, 4, 1, 128, 16, [70001], 7, None), (BF16, 8, 1, 64, 64, [33000, 5], 7, [7, 3]), (F32, 2, 1, 128, 32, [40000], 7, [5]), (BF16, 32, 8, 128, 16, [4000, 17, 901, 2500], 64, [64, 30, 7, 12]),
     (BF16, 40, 4, 128, 128, [3000, 5000], 40, [40, 17]), (BF16, 8, 2, 64, 16, list(range(0, 640, 2)), 7, [b % 8 for b in range(320)]), (BF16, 16, 1, 128, 16, [1000] * 50, 7, None),
-    (F32, 8, 4, 64, 16, [700] * 20, 7, [3] * 20), (BF16, 64, 2, 128, 16, [9000, 2000], 256, [256, 100])])
+    (F32, 8, 4, 64, 16, [700] * 20, 7, [3] * 20), (F32, 8, 2, 64, 64, [33000, 5], 7, [7, 3]), (BF16, 64, 2, 128, 16, [9000, 2000], 256, [256, 100])])
 def test_long_contexts_and_large_batches(dtype, Hq, Hkv, Dh, ps, lens, N, n_nodes):
     B = len(lens)
     ts = context(Nmax=N, B=B, dtype=dtype)
