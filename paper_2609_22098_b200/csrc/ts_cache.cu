@@ -206,7 +206,8 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
     const int base = count - taken;
     if (WHERE == 0) cooperative_groups::this_cluster().sync();
     else __syncthreads();
-    for (int b = me; b < a.B; b += warps) {
+    const bool gives = all >> 32 != 0;   // (the same in all CTAs)
+    for (int b = me; gives && b < a.B; b += warps) {
       if (a.seq_len[b] >= 0) continue;
       // (held[b] may be written by CTA 0 below once all have passed the second barrier only)
       const int n = pages_held(a, b), at = base + (int)(pre[b] >> 32);
@@ -217,8 +218,10 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
         if (at + c < a.d.n_pages) a.free_pages[at + c] = page;
       }
     }
-    if (WHERE == 0) cooperative_groups::this_cluster().sync();
-    else __syncthreads();
+    if (gives) {
+      if (WHERE == 0) cooperative_groups::this_cluster().sync();
+      else __syncthreads();
+    }
     if (blockIdx.x == 0) {
 #pragma unroll
       for (int k = 0; k < OWN; ++k) {
@@ -295,15 +298,19 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) {
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// x / s to the nearest whole number, the even one of two as near, without a division (eight a lane were most of the kernel's
-// instructions): the product with 1/s is off by 2^-23 of it, so its rounding is the result or next to it; what is left of x
-// says which, exactly, because it is a multiple of x's last place and no larger than x.
+// WHOLE + x / s to the nearest whole number, the even one of two as near, without a division or a conversion (which run at a
+// quarter of the rate): at 1.5 * 2^23 a sum is rounded to whole numbers, and the number stands in its last bits.  The product
+// with 1/s is off by 2^-23 of it, so what it is rounded to is the result or next to it; what is left of x says which, exactly,
+// because it is a multiple of x's last place and no larger than x.  (Beyond 2^22 the sum is no whole number apart, and no matter:
+// codes end at 7.)
+constexpr float WHOLE = 12582912.f;
 __device__ __forceinline__ float nearest_code(float x, float s, float inv) {
-  const float c = rintf(x * inv), r = fmaf(-c, s, x), h = 0.5f * s;
-  const bool odd = (int)c & 1;
-  if (r > h || (r == h && odd)) return c + 1.f;
-  if (r < -h || (r == -h && odd)) return c - 1.f;
-  return c;
+  float t = fmaf(x, inv, WHOLE);
+  const float r = fmaf(WHOLE - t, s, x);
+  // more than half of s is left, or just half and the number is odd: magnitudes compare as integers
+  const unsigned left = __float_as_uint(r) & 0x7FFFFFFFu, odd = __float_as_uint(t) & 1u;
+  if (left + odd > __float_as_uint(0.5f * s)) t += copysignf(1.f, r);
+  return fminf(fmaxf(t, WHOLE - 8.f), WHOLE + 7.f);
 }
 
 template <typename T, int Dh>
@@ -325,22 +332,20 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
   }
   float x[8];
   const int exp = is_v ? a.v_exp : a.k_exp;
-  float top = 0.f;
-  bool fine = true;
+  unsigned most = 0u;   // largest magnitude, as an integer: what is not finite is larger than all that is
   if (slot >= 0) {
     load8(reinterpret_cast<const T*>(is_v ? a.v : a.k) + row * (is_v ? a.ldv : a.ldk) + (long long)h * Dh + 8 * c, x);
     const float f = __uint_as_float((unsigned)(127 - exp) << 23);   // 2^-exp
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       x[i] *= f;
-      fine = fine && isfinite(x[i]);
-      top = fmaxf(top, fabsf(x[i]));
+      most = max(most, __float_as_uint(x[i]) & 0x7FFFFFFFu);
     }
   }
   // whether all of the row's head is finite: the ballot's bits of this group of lanes
   const unsigned group = LANES == 32 ? ~0u : 0xFFFFu << (threadIdx.x & 16);
-  fine = (__ballot_sync(~0u, fine) & group) == group;
-  top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+  const bool fine = (__ballot_sync(~0u, most < 0x7F800000u) & group) == group;
+  const float top = __uint_as_float(max(most, __shfl_xor_sync(~0u, most, 1)));
   if (slot < 0) return;
   // The quotient by IEEE division, rounded once more: a value half-way between two scales has few enough bits to be a quotient
   // that fp32 holds, and no other quotient rounds to it, so the result is the rounding of the exact quotient.
@@ -353,21 +358,22 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
   uint32_t r;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)byte));
   float s = __half2float(__low2half(as_half2(r)));
-  uint32_t word = 0x88888888u;
+  uint32_t word = 0u;   // codes without their offset of 8: four bits of the number
   if (!fine) byte = SCALE_NAN;
   else if (s > 0.f) {
     const float inv = __frcp_rn(s);
-    word = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float code = fminf(fmaxf(nearest_code(x[i], s, inv), -8.f), 7.f);
-      word |= (unsigned)((int)code + 8) << (4 * (i / 2 + 4 * (i % 2)));
-      x[i] = code;
+      const float t = nearest_code(x[i], s, inv);
+      const int at = 4 * (i / 2 + 4 * (i % 2));
+      word |= (__float_as_uint(t) << at) & (0xFu << at);
+      x[i] = t - WHOLE;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = 0.f;
   }
+  word ^= 0x88888888u;
   const int page = slot / a.d.ps, in = slot - page * a.d.ps, tau = in % CACHE_BLOCK;
   unsigned char* blk = a.pool + block_offset(a.d, page, in / CACHE_BLOCK, h);
   const int g = c >> 1;

@@ -83,6 +83,29 @@ def test_append_writes_the_oracles_bytes(dtype, Hkv, Dh, ps, rows, ld, exps):
     assert torch.equal(again, pool)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_append_rounds_codes_to_the_nearest_even(dtype):
+    """Values at every border between two codes and a last place to either side, for all scales."""
+    Dh, ps = 64, 16
+    scales = [float(x) for x in torch.arange(1, 127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()]
+    near = []
+    for s in scales:
+        t = torch.tensor([7 * s] + [(c + 0.5) * s for c in range(-8, 7)], dtype=torch.float64).to(dtype)   # (borders of bf16 values are rounded: they are near one then)
+        up, down = (torch.nextafter(t, torch.full_like(t, d)) for d in (float("inf"), float("-inf")))
+        up[0] = down[0] = t[0]
+        near += [t, up, down, -t]
+    x = torch.stack(near).reshape(-1, 1, Dh)
+    rows = x.shape[0]
+    ts, lay = context(dtype=dtype), CacheLayout(1, 1, Dh, ps, -(-rows // ps), 4, dtype)
+    start = np.zeros(lay.pool_shape(), np.uint8)
+    pool = torch.from_numpy(start.copy()).cuda()
+    k_val, v_val = (torch.zeros(rows, 1, Dh, dtype=dtype, device="cuda") for _ in range(2))
+    ts.cache_append(lay, x.cuda(), x.flip(0).contiguous().cuda(), i32(range(rows)), pool, k_val, v_val)
+    kv, vv = oc.append(start, ps, list(range(rows)), x.double().numpy(), x.flip(0).double().numpy(), 0, 0)
+    assert np.array_equal(pool.cpu().numpy(), start)
+    assert np.array_equal(k_val.double().cpu().numpy(), kv) and np.array_equal(v_val.double().cpu().numpy(), vv)
+
+
 def test_append_beyond_32_bit_offsets():
     Dh, ps = 128, 16
     pages = (5 << 30) // (18 * Dh)
