@@ -49,8 +49,8 @@ __device__ __forceinline__ int unit_set(const AttnArgs& a, int b, AttnUnit& u) {
   u.b = b; u.seq = a.seq_len[b];
   u.rows = request_rows(a.n_nodes, b, a.rcap);
   if (u.seq < 0) { u.n = 0; u.nq = 0; return 0; }
-  const long long end = min((long long)u.seq + u.rows, (long long)a.d.cols * a.d.ps);   // (no page beyond the table's)
-  u.n = (int)max(1ll, (end + S::TOK - 1) / S::TOK);
+  const unsigned end = min((unsigned)u.seq + (unsigned)u.rows, (unsigned)a.d.cols * (unsigned)a.d.ps);   // (no page beyond the table's)
+  u.n = max(1u, (end + S::TOK - 1) / S::TOK);
   u.nq = (u.rows * a.d.G + S::QT - 1) / S::QT;
   return a.d.Hkv * u.nq;
 }
@@ -96,7 +96,9 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, int& first, long lon
   at -= sum; nth -= cnt;
   __syncthreads();
   long long total = 0, all = 0;
-  for (int w = 0; w < THREADS / 32; ++w) {
+  const int warps = min(THREADS / 32, (a.B + 32 * per - 1) / (32 * per));   // that have requests
+#pragma unroll 1
+  for (int w = 0; w < warps; ++w) {
     if (w < warp) { at += wsum[w][0]; nth += wsum[w][1]; }
     total += wsum[w][0]; all += wsum[w][1];
   }
@@ -112,7 +114,7 @@ __device__ bool attn_locate(const AttnArgs& a, AttnUnit& u, int& first, long lon
     long long x = (side ? x1 : x0) - at, k = nth;
     if (x < 0 || x >= sum) continue;
     for (int b = b0;; ++b) {
-      const long long units = unit_set<S>(a, b, u), len = u.n + S::LEAD;
+      const long long units = per == 1 ? (long long)a.d.Hkv * u.nq : unit_set<S>(a, b, u), len = u.n + S::LEAD;   // (one request a thread: u has it)
       if (x < units * len) {
         u.v = (int)divide(x, len);
         x -= u.v * len;   // within the unit

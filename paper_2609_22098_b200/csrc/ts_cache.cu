@@ -68,9 +68,9 @@ struct ReservePlan { int rows, held, need, start; bool granted, release; };
 __device__ __forceinline__ int pages_needed(const ReserveArgs& a, int b) {
   const int n = a.seq_len[b];
   if (n < 0) return -1;
-  const long long end = (long long)n + request_rows(a.n_nodes, b, a.rcap);
-  const long long need = (end + a.d.ps - 1) / a.d.ps;
-  return need > a.d.cols ? a.d.cols + 1 : (int)need;
+  const unsigned end = (unsigned)n + (unsigned)request_rows(a.n_nodes, b, a.rcap);   // below 2^31 + 257
+  const unsigned need = (end + (unsigned)a.d.ps - 1u) / (unsigned)a.d.ps;           // (a division of 64 bits is a call)
+  return need > (unsigned)a.d.cols ? a.d.cols + 1 : (int)need;
 }
 __device__ __forceinline__ int pages_held(const ReserveArgs& a, int b) { return min(max(a.held[b], 0), a.d.cols); }
 __device__ __forceinline__ int pages_taken(const ReserveArgs& a, int b) {
@@ -83,8 +83,8 @@ __device__ __forceinline__ long long pages_of(const ReserveArgs& a, int b) {
   return (long long)pages_taken(a, b) + (a.seq_len[b] < 0 ? (long long)pages_held(a, b) << 32 : 0ll);
 }
 __device__ __forceinline__ long long add_pages(long long x, long long y) {
-  const long long top = 0x7FFFFFFFll;
-  return min((x & 0xFFFFFFFFll) + (y & 0xFFFFFFFFll), top) | (min((x >> 32) + (y >> 32), top) << 32);
+  const unsigned top = 0x7FFFFFFFu;
+  return (long long)((unsigned long long)min((unsigned)(x >> 32) + (unsigned)(y >> 32), top) << 32 | min((unsigned)x + (unsigned)y, top));
 }
 
 // Exclusive running sums over requests, in shared memory; returns the total.
@@ -92,7 +92,7 @@ __device__ long long reserve_scan(const ReserveArgs& a, long long* pre) {
   __shared__ long long wsum[RES_THREADS / 32];
   const int per = (a.B + RES_THREADS - 1) / RES_THREADS, b0 = threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long sum = 0;
-  for (int b = b0; b < min(b0 + per, a.B); ++b) sum = add_pages(sum, pages_of(a, b));
+  for (int b = b0; b < min(b0 + per, a.B); ++b) sum = add_pages(sum, pre[b] = pages_of(a, b));
   long long inc = sum;
   for (int o = 1; o < 32; o <<= 1) {
     const long long v = __shfl_up_sync(~0u, inc, o);
@@ -108,8 +108,9 @@ __device__ long long reserve_scan(const ReserveArgs& a, long long* pre) {
     all = add_pages(all, wsum[w]);
   }
   for (int b = b0; b < min(b0 + per, a.B); ++b) {
+    const long long mine = pre[b];
     pre[b] = at;
-    at = add_pages(at, pages_of(a, b));
+    at = add_pages(at, mine);
   }
   __syncthreads();
   return all;
@@ -137,9 +138,9 @@ __device__ void reserve_rows(const ReserveArgs& a, int b, const ReservePlan& p, 
   for (int i = lane; i < a.rcap; i += 32) {
     int slot = -1;
     if (p.granted && i < p.rows) {
-      const int pos = first + i, c = pos / a.d.ps;
+      const int pos = first + i, c = (unsigned)pos / (unsigned)a.d.ps;
       const int page = c < p.held ? row[c] : a.free_pages[count - 1 - (p.start + c - p.held)];
-      if ((unsigned)page < (unsigned)a.d.n_pages) slot = page * a.d.ps + pos % a.d.ps;
+      if ((unsigned)page < (unsigned)a.d.n_pages) slot = page * a.d.ps + (pos - c * a.d.ps);
     }
     a.slot_map[(size_t)b * a.rcap + i] = slot;
   }
@@ -266,7 +267,7 @@ static cudaError_t launch_reserve(ts_ctx* ctx, const ReserveArgs& a, cudaStream_
 // values): 16.7 us for 50 MB, 3 TB/s; the trees of 32 requests in bf16 9 us for 11 MB.  Bound by issue and by the ramp of so
 // short a kernel; two rows a lane, side by side, took as long.
 // ------------------------------------------------------------------------------------------------
-constexpr int APP_THREADS = 256;
+constexpr int APP_THREADS = 128;   // (128, 256, 512: the chunks below take 12.8, 13.1, 14.5 us in a row)
 
 struct AppendArgs {
   CacheDims d;
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
   int slot = -1, h = 0;
   long long row = 0;
   if (item < a.items) {
-    row = item / a.d.Hkv;
+    row = a.items >> 31 ? item / a.d.Hkv : (long long)((unsigned)item / (unsigned)a.d.Hkv);   // (a division of 64 bits is a call)
     h = (int)(item - row * a.d.Hkv);
     slot = a.slot_map[row];
     if (slot >= (long long)a.d.n_pages * a.d.ps) slot = -1;
@@ -374,7 +375,7 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
     for (int i = 0; i < 8; ++i) x[i] = 0.f;
   }
   word ^= 0x88888888u;
-  const int page = slot / a.d.ps, in = slot - page * a.d.ps, tau = in % CACHE_BLOCK;
+  const int page = (unsigned)slot / (unsigned)a.d.ps, in = slot - page * a.d.ps, tau = in % CACHE_BLOCK;
   unsigned char* blk = a.pool + block_offset(a.d, page, in / CACHE_BLOCK, h);
   const int g = c >> 1;
   if (is_v) {
@@ -426,14 +427,15 @@ __global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs
     long long f = -1, t = -1;
     if (i < n) {
       const int node = a.acc_node[(size_t)b * a.D + i];
-      const long long src = (long long)seq + 1 + node, dst = (long long)seq + 1 + i, room = (long long)a.d.cols * a.d.ps;
+      const unsigned ps = a.d.ps, room = (unsigned)a.d.cols * ps, src = (unsigned)seq + 1u + (unsigned)node, dst = (unsigned)seq + 1u + (unsigned)i;   // (below 2^31 + 257)
       if (node >= 0 && node < a.N && src != dst && src < room && dst < room) {
         const int* row = a.table + (size_t)b * a.d.cols;
-        f = block_offset(a.d, row[src / a.d.ps], (int)(src % a.d.ps) / CACHE_BLOCK, 0);
-        t = block_offset(a.d, row[dst / a.d.ps], (int)(dst % a.d.ps) / CACHE_BLOCK, 0);
+        const unsigned cs = src / ps, ct = dst / ps;
+        f = block_offset(a.d, row[cs], (src - cs * ps) / CACHE_BLOCK, 0);
+        t = block_offset(a.d, row[ct], (dst - ct * ps) / CACHE_BLOCK, 0);
         if (f < 0 || t < 0) f = t = -1;
       }
-      ft[i] = (int)(src % CACHE_BLOCK); tt[i] = (int)(dst % CACHE_BLOCK);   // (pages are whole blocks)
+      ft[i] = src % CACHE_BLOCK; tt[i] = dst % CACHE_BLOCK;   // (pages are whole blocks)
     }
     from[i] = f; to[i] = t;
   }
