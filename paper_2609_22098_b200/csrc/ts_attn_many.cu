@@ -10,11 +10,11 @@
 // converted keys and values; with fewer they take the same rows and every other step, and their halves are joined at the end.
 // Either way one group's exponentials run beside the other's matrix products.
 //
-// Trees of 120 to 256 nodes of 8 requests behind 2,000 to 16,000 tokens, 32 query heads on 4 of 128 channels: 274 us, 0.71 PFLOP/s, 44 % of
-// what a large matrix product reaches.  Trees of 8 to 30 nodes of 32 requests behind 500 to 6,000 tokens, 8 kv heads: 114 us, 1.1 TB/s.  A
-// step takes 2.2 us with two tiles and 1.5 with one; its products keep the tensor cores busy for 39 % of the time and its
-// exponentials their unit for 39 %.  What bounds it is the chain of a tile (scores, their largest, weights, products) and the
-// waits between its links, which two groups cover in part; with one tile the converters (64 KB of fp16 a step) are as busy.
+// Trees of 120 to 256 nodes of 8 requests behind 2,000 to 16,000 tokens, 32 query heads on 4 of 128 channels: 236 us, 0.83 PFLOP/s, 51 % of
+// what a large matrix product reaches.  Trees of 8 to 30 nodes of 32 requests behind 500 to 6,000 tokens, 8 kv heads: 98 us, 1.3 TB/s.
+// What bounds it is the chain of a tile (scores, their largest, weights, product with V, then the next scores, which need the
+// weights' columns) and the waits between its links, which two groups cover in part; with one tile the converters (64 KB of
+// fp16 a step) are as busy.
 #include <string.h>
 
 #include "ts_attn.cuh"
@@ -24,9 +24,10 @@ namespace ts {
 
 constexpr int MANY_TOKENS = 128;                  // a step
 constexpr int MANY_QT = 256;
-// A lead of four steps (trees of 32 requests behind 500 to 6,000 tokens, us, with leads of 0, 2, 4, 6, 9: 161, 135, 122, 125, 128).  Steps
-// with one and with two tiles count alike: 1.5 and 2.2 us, but what they wait for is the same (counted as 2 to 3: 298 us for
-// 281 where both occur).
+// A lead of four steps (trees of 32 requests behind 500 to 6,000 tokens and the crowded trees above, us, with leads of 2, 3, 4, 6: 105
+// and 247, 100 and 242, 98 and 236, 101 and 236; without one the trees took a third longer).  Steps
+// with one and with two tiles count alike: the former are shorter, but what they wait for is the same (counted as 2 to 3 they
+// took the crowded trees 6 % longer).
 using ManyShape = AttnShape<MANY_QT, MANY_TOKENS, 4>;
 constexpr int MANY_SOFT = 16, MANY_CONV = 4;      // warps (converters: half for K, half for V)
 constexpr int MANY_CT = MANY_CONV / 2 * 32;       // threads of either kind
@@ -89,7 +90,7 @@ __device__ __forceinline__ void soft_sync() { asm volatile("bar.sync 1, %0;" ::"
 __device__ __forceinline__ void pair_sync(int quad) { asm volatile("bar.sync %0, 64;" ::"r"(2 + quad) : "memory"); }
 
 // a CTA's piece: its first unit, the number of its first step there, its steps
-struct ManyPiece { AttnUnit u; long long steps; int first, spare; };
+struct ManyPiece { AttnUnit u; int steps, first; };
 
 struct ManyShared {
   ManyPiece piece;
@@ -100,28 +101,33 @@ struct ManyShared {
   float f[2][128];                       // factors of the rows' scores, by tile
   float top[2][2][128];                  // by group and half: largest scores of a step; at a unit's end the rows' references
   float sum[2][2][128];                  // and sums
+  AttnUnit unit[MANY_SOFT];              // what a softmax warp works on
 };
 
-// Every role reads its own copy of the piece: kept in registers across the parting of the roles it was spilled in all of them.
-__device__ __forceinline__ ManyPiece my_piece(const ManyShared& sh) {
-  ManyPiece p;
-  constexpr int W = sizeof(ManyPiece) / 4;
-  static_assert(sizeof(ManyPiece) % 4 == 0, "words");
+// A copy from shared memory that is made where it stands.  Every role reads its own copy of the piece (kept in registers across the
+// parting of the roles it was spilled in all of them), and the softmax warps read their unit again behind its steps.  Spilled
+// words of 768 threads do not fit beside so much shared memory in L1: 220 bytes a thread made trees 14 % slower.
+template <class T>
+__device__ __forceinline__ T copy_of(const T& in) {
+  T out;
+  constexpr int W = sizeof(T) / 4;
+  static_assert(sizeof(T) % 4 == 0, "words");
   uint32_t w[W];
 #pragma unroll
-  for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const volatile uint32_t*>(&sh.piece)[i];
-  memcpy(&p, w, sizeof(p));
-  return p;
+  for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const volatile uint32_t*>(&in)[i];
+  memcpy(&out, w, sizeof(out));
+  return out;
 }
 
 // The steps of a CTA's piece that belong to one unit: n from j0 on; `left` steps of the piece are to be taken.
 struct ManySegment { int h, first, j0, n, two; bool whole; };
-__device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const AttnUnit& u, int j0, long long left) {
+__device__ __forceinline__ int many_first(const AttnUnit& u) { return u.v % u.nq * MANY_QT; }
+__device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const AttnUnit& u, int j0, int left) {
   ManySegment s;
   s.h = u.v / u.nq;
-  s.first = (u.v - s.h * u.nq) * MANY_QT;
+  s.first = many_first(u);
   s.j0 = j0;
-  s.n = (int)min((long long)(u.n - j0), left);
+  s.n = min(u.n - j0, left);
   s.two = u.rows * a.d.G - s.first > 128;
   s.whole = s.n == u.n;
   return s;
@@ -134,10 +140,10 @@ __device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const Att
 template <int Dh>
 __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw) {
   using P = ManyPlan<Dh>;
-  const ManyPiece piece = my_piece(sh);
+  const ManyPiece piece = copy_of(sh.piece);
   AttnUnit u = piece.u;
   constexpr uint32_t BLK = cache_block_bytes(Dh);
-  const int lane = threadIdx.x & 31, per = a.d.ps / CACHE_BLOCK, half_steps = 2 * (int)piece.steps;
+  const int lane = threadIdx.x & 31, per = a.d.ps / CACHE_BLOCK, half_steps = 2 * piece.steps;
   int j = piece.first + (lane >> 3), mine = lane >> 2;   // the lane's step within its unit, its half-step in all
   int page = -1, inner = 0;
   auto look_up = [&]() {
@@ -275,7 +281,7 @@ struct ValuePart {
 template <class Part, int Dh>
 __device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* raw, unsigned char* stages, uint64_t* full, uint64_t (*free)[2], int tid) {
   using P = ManyPlan<Dh>;
-  const ManyPiece piece = my_piece(sh);
+  const ManyPiece piece = copy_of(sh.piece);
   AttnUnit u = piece.u;
   const int lane = threadIdx.x & 31;
   volatile int* abort = (volatile int*)&sh.abort;
@@ -283,7 +289,7 @@ __device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* r
   uint32_t phase = 0;
   uint32_t used = 0;   // who read the stages last: bits of groups, by stage
   uint32_t turn = 0;   // parity of the uses so far, a bit for each group and stage
-  long long left = piece.steps;
+  int left = piece.steps;
   for (int j0 = piece.first; left > 0; j0 = 0) {
     const ManySegment s = many_segment(a, u, j0, left);
     left -= s.n;
@@ -324,7 +330,7 @@ __device__ void many_convert(const AttnArgs& a, ManyShared& sh, unsigned char* r
 template <int Dh>
 __device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* smem) {
   using P = ManyPlan<Dh>;
-  const ManyPiece piece = my_piece(sh);
+  const ManyPiece piece = copy_of(sh.piece);
   AttnUnit u = piece.u;
   volatile int* abort = (volatile int*)&sh.abort;
   constexpr uint32_t id_s = (1u << 4) | ((uint32_t)(MANY_TOKENS >> 3) << 17) | ((128u >> 4) << 24);              // D = f32, A = B = f16, M = 128; B K-major: keys
@@ -332,7 +338,7 @@ __device__ void many_issue(const AttnArgs& a, ManyShared& sh, unsigned char* sme
   const uint64_t qd = smem_desc(smem_u32(smem + P::Q), 16u, 1024u), kd = smem_desc(smem_u32(smem + P::K), 16u, 1024u), vd = smem_desc(smem_u32(smem + P::V), P::SLAB, 1024u);
   uint32_t weights = 0, segments = 0;   // weights: parity of the waits for each group's
   int base = 0;                         // steps before this segment
-  long long left = piece.steps;
+  int left = piece.steps;
   for (int j0 = piece.first; left > 0; j0 = 0, ++segments) {
     const ManySegment s = many_segment(a, u, j0, left);
     left -= s.n;
@@ -530,7 +536,7 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], SoftRow& row, uin
 template <int Dh>
 __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* smem) {
   using P = ManyPlan<Dh>;
-  const ManyPiece piece = my_piece(sh);
+  const ManyPiece piece = copy_of(sh.piece);
   AttnUnit u = piece.u;
   volatile int* abort = (volatile int*)&sh.abort;
   // group, half of a step's tokens, row of the tile (a warp reaches the 32 rows of its number modulo 4)
@@ -541,17 +547,19 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
   uint32_t count = 0;   // products of this group
   int base = 0;
   bool alive = true, apart = false;   // apart: the groups had tiles of their own in the unit before
-  long long left = piece.steps;
+  int left = piece.steps;
   for (int j0 = piece.first; left > 0; j0 = 0) {
-    const ManySegment s = many_segment(a, u, j0, left);
+    ManySegment s = many_segment(a, u, j0, left);
     left -= s.n;
-    const int idx = s.first + (s.two ? grp * 128 : 0) + row, i = tree_row(a, idx);
+    int idx = s.first + (s.two ? grp * 128 : 0) + row;
     // The warps of 32 rows load a share each, of their own tile or of the shared one, which the first group's products of the
     // unit before may still read.
     if (!s.two && apart) soft_sync();
     apart = s.two;
     load_queries<Dh>(a, u, s.h, idx, s.two ? 16 * hh : 16 * grp + 8 * hh, s.two ? 16 : 8, smem + P::Q + (s.two ? grp * P::TILE : 0), row, sh.f[s.two ? grp : 0]);
     fence_async_smem();
+    if (lane == 0) sh.unit[warp] = u;
+    const int seq = u.seq;
     __syncwarp();
     if (lane == 0) {   // (sixteen arrivals: of all warps, or twice of the group's own)
       mbar_arrive(&sh.bars.q_full[grp]);
@@ -570,10 +578,12 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
       const int tok0 = (s.j0 + j) * MANY_TOKENS;
       const unsigned here = sh.present[(base + j) % MANY_PRESENT] >> (4 * hh) & 0xFu;
       uint32_t on[2] = {~0u, ~0u}, x[32];
-      if (tok0 > u.seq - MANY_TOKENS || here != 0xFu) {
+      if (tok0 > seq - MANY_TOKENS || here != 0xFu) {
+        const AttnUnit k = copy_of(sh.unit[warp]);
+        const int i = tree_row(a, many_first(k) + (s.two ? grp * 128 : 0) + row);
 #pragma unroll
         for (int c = 0; c < 2; ++c)
-          on[c] = ((here >> (2 * c) & 1u ? 0xFFFFu : 0u) | (here >> (2 * c + 1) & 1u ? 0xFFFF0000u : 0u)) & sees32(a, u.b, i, tok0 + 64 * hh + 32 * c - u.seq, u.rows);
+          on[c] = ((here >> (2 * c) & 1u ? 0xFFFFu : 0u) | (here >> (2 * c + 1) & 1u ? 0xFFFF0000u : 0u)) & sees32(a, k.b, i, tok0 + 64 * hh + 32 * c - seq, k.rows);
       }
       float top = -INFINITY;
       if (alive) {
@@ -615,6 +625,9 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
       ++done;
     }
     // ---- results: by group and half, channels of the group's own tile or of the rows that the groups share
+    u = copy_of(sh.unit[warp]);
+    s = many_segment(a, u, j0, s.n);
+    idx = s.first + (s.two ? grp * 128 : 0) + row;
     if (alive && done > 0) alive = __all_sync(~0u, mbar_wait(&sh.bars.o_full[grp], (count - 1u) & 1u, abort, nullptr, a.limit));
     sh.top[grp][hh][row] = my.m == -INFINITY ? -INFINITY : my.ref;
     sh.sum[grp][hh][row] = my.l;
@@ -634,62 +647,59 @@ __device__ void many_softmax(const AttnArgs& a, ManyShared& sh, unsigned char* s
     if (!alive || *abort) sum = NAN;
     tc_fence_after();
     const int rows = u.rows * a.d.G;
-    const size_t slot = ((size_t)blockIdx.x * 2 + (s.j0 > 0 ? 0 : 1)) * MANY_QT + (s.two ? grp * 128 : 0) + row;
+    const int slot = ((int)blockIdx.x * 2 + (s.j0 > 0 ? 0 : 1)) * MANY_QT + (s.two ? grp * 128 : 0) + row;
     const float inv = s.whole ? row_inv(sum) * a.vo : 1.f;
     const int n = s.two ? Dh / 64 : 1, c_lo = (s.two ? hh : grp * 2 + hh) * n, c_hi = min(c_lo + n, Dh / 32);   // groups of 32 channels
-#pragma unroll 1
-    for (int c = c_lo; c < c_hi; ++c) {
-      uint32_t x[32];
-      tmem_ld32(to + (s.two ? grp * Dh : 0) + 32 * c, x);
-      tmem_ld32_wait(x);
-#pragma unroll
-      for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(w0 * __uint_as_float(x[k]) * inv);
-      if (other) {
-        uint32_t y[16];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          tmem_ld16_issue(to + Dh + 32 * c + 16 * half, y);
-          tmem_ld16_wait(y);
-#pragma unroll
-          for (int k = 0; k < 16; ++k) x[16 * half + k] = __float_as_uint(fmaf(w1 * inv, __uint_as_float(y[k]), __uint_as_float(x[16 * half + k])));
-        }
-      }
-      // through the stage in pieces of 16 bytes, so that rows leave in whole lines: bf16 in one round, fp32 in one or two
-      constexpr int ROOM = Dh / 16;   // pieces of a staged row
-      const int bits = s.whole || ROOM == 4 ? 2 : 3, rounds = s.whole ? 1 : 8 >> bits;
-#pragma unroll 1
-      for (int rd = 0; rd < rounds; ++rd) {
-        auto put = [&](int k, uint4 v) { *reinterpret_cast<uint4*>(stage + lane * Dh + ((k ^ (lane & (ROOM - 1))) << 4)) = v; };
-        if (s.whole) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint32_t w[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(x[8 * k + 2 * q]), __uint_as_float(x[8 * k + 2 * q + 1]));
-              w[q] = *reinterpret_cast<const uint32_t*>(&h2);
-            }
-            put(k, make_uint4(w[0], w[1], w[2], w[3]));
-          }
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (ROOM == 8 || k / 4 == rd) put(k & (ROOM - 1), make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]));
-        }
-        __syncwarp();
-        for (int e = lane; e < 32 << bits; e += 32) {
-          const int r = e >> bits, k = e - (r << bits), id = idx - lane + r;
-          if (id >= rows) break;   // (rows rise with e)
-          const uint4 t = *reinterpret_cast<const uint4*>(stage + r * Dh + ((k ^ (r & (ROOM - 1))) << 4));
-          if (s.whole) reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row(a, u.b, s.h, id) + 32 * c)[k] = t;
-          else reinterpret_cast<uint4*>(a.part + (slot - lane + r) * Dh + 32 * c)[rd * 4 + k] = t;
-        }
-        __syncwarp();
-      }
-    }
     if (idx < rows && hh == 0 && (s.two || grp == 0)) {
       if (!s.whole) { a.part_ml[2 * slot] = top; a.part_ml[2 * slot + 1] = sum; }
       else if (a.lse) a.lse[lse_row(a, u.b, s.h, idx)] = row_lse(top, sum);
+    }
+    // through the stage in pieces of 16 bytes, so that rows leave in whole lines: 32 channels as bf16 or fp32, 16 as fp32 where a
+    // staged row has no more room
+    constexpr int ROOM = Dh / 16;   // pieces of a staged row
+    const int bits = s.whole || ROOM == 4 ? 2 : 3;
+    const bool halves = !s.whole && ROOM == 4;
+#pragma unroll 1
+    for (int c = 2 * c_lo; c < 2 * c_hi; ++c) {   // (16 channels at a time: 32 with the other group's do not fit the registers)
+      uint32_t x[16];
+      tmem_ld16_issue(to + (s.two ? grp * Dh : 0) + 16 * c, x);
+      tmem_ld16_wait(x);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(w0 * __uint_as_float(x[k]) * inv);
+      if (other) {
+        uint32_t y[16];
+        tmem_ld16_issue(to + Dh + 16 * c, y);
+        tmem_ld16_wait(y);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(fmaf(w1 * inv, __uint_as_float(y[k]), __uint_as_float(x[k])));
+      }
+      auto put = [&](int k, uint4 v) { *reinterpret_cast<uint4*>(stage + lane * Dh + ((k ^ (lane & (ROOM - 1))) << 4)) = v; };
+      if (s.whole) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t w[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(x[8 * k + 2 * q]), __uint_as_float(x[8 * k + 2 * q + 1]));
+            w[q] = *reinterpret_cast<const uint32_t*>(&h2);
+          }
+          put(2 * (c & 1) + k, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) put((4 * (c & 1) + k) & (ROOM - 1), make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]));
+      }
+      if (!halves && !(c & 1)) continue;
+      __syncwarp();
+      const int ch = halves ? 16 * c : 16 * (c & ~1);   // the first staged channel
+      for (int e = lane; e < 32 << bits; e += 32) {
+        const int r = e >> bits, k = e - (r << bits), id = idx - lane + r;
+        if (id >= rows) break;   // (rows rise with e)
+        const uint4 t = *reinterpret_cast<const uint4*>(stage + r * Dh + ((k ^ (r & (ROOM - 1))) << 4));
+        if (s.whole) reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + out_row(a, u.b, s.h, id) + ch)[k] = t;
+        else reinterpret_cast<uint4*>(a.part + (size_t)(slot - lane + r) * Dh + ch)[k] = t;
+      }
+      __syncwarp();
     }
     tc_fence_before();
     // all have read the sums and left the stages, before the next unit's products and queries overwrite them
@@ -728,7 +738,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (threadIdx.x == 0) { sh.piece.u = u; sh.piece.first = first; sh.piece.steps = steps; }
+  if (threadIdx.x == 0) { sh.piece.u = u; sh.piece.first = first; sh.piece.steps = (int)steps; }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
