@@ -126,6 +126,7 @@ extern "C" int32_t ts_create(const ts_config* cfg, ts_ctx** out) {
   if (e == cudaSuccess) e = walk_setup(ctx);
   if (e == cudaSuccess) e = expand_setup(ctx);
   if (e == cudaSuccess) e = attn_setup(ctx);
+  if (e == cudaSuccess) e = cache_setup(ctx);
   if (e != cudaSuccess) { cudaFree(ctx->d_table); delete (Prof*)ctx->prof; delete ctx; return set_cuda_error("ts_create", e); }
   *out = ctx;
   return TS_OK;

@@ -398,14 +398,16 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
 // Commit.  A warp per (request, layer, head) holds the bytes of all moved rows before it writes one: sources and targets of
 // a path overlap.  The CTAs of a request form a cluster, whose barrier lets the new length overwrite the old.  Bound by latency
 // (nodes, table, bytes, then the writes): paths of up to eight rows of 32 requests, 12 layers of 8 heads, 8.5 us for 4 MB; of one
-// request with 36 layers 11 us for 0.6 MB.
+// request with 36 layers 5.7 us on the device for 0.6 MB.
 // ------------------------------------------------------------------------------------------------
-constexpr int COM_THREADS = 1024;   // at most: a warp for each layer and head of a request where 256 are enough
-constexpr int COM_CLUSTER = 8;
+constexpr int COM_THREADS = 1024;   // at most: a warp for each layer and head of a request
+// CTAs of a request: eight, and sixteen where a warp would have to take more than one layer and head (one request with 36 layers of
+// 8 heads: 10.9 and 5.7 us, with 12 layers 5.2 and 5.0) and the device has clusters of sixteen.
+constexpr int COM_CLUSTER = 8, COM_LARGE = 16;
 
 struct CommitArgs {
   CacheDims d;
-  int B, D, N, layers;
+  int B, D, N, layers, cluster;
   size_t layer_stride;
   unsigned char* pool;
   const int *table, *seq_len, *acc_len, *acc_node;
@@ -419,7 +421,7 @@ __global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs
   __shared__ int ft[DMAX], tt[DMAX];           // tokens within the blocks
   pdl_wait();
   pdl_launch_dependents();
-  const int b = blockIdx.x / COM_CLUSTER, part = blockIdx.x % COM_CLUSTER;
+  const int b = blockIdx.x / a.cluster, part = blockIdx.x - b * a.cluster;
   const int lane = threadIdx.x & 31;
   const int seq = a.seq_len[b], n = seq < 0 ? 0 : min(max(a.acc_len[b], 0), a.D);
   if (threadIdx.x < DMAX) {
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs
   __syncthreads();
   // a lane's word of a token: K codes, then V codes; its byte: K scales, then V scales
   constexpr int W = Dh / 8;   // words of K codes (as many of V)
-  const int warps = COM_CLUSTER * (blockDim.x / 32);
+  const int warps = a.cluster * (blockDim.x / 32);
   for (int item = part * (blockDim.x / 32) + (threadIdx.x >> 5); item < a.layers * a.d.Hkv; item += warps) {
     const int layer = item / a.d.Hkv, h = item - layer * a.d.Hkv;
     unsigned char* base = a.pool + (size_t)layer * a.layer_stride + (size_t)h * (a.d.ps / CACHE_BLOCK) * cache_block_bytes(Dh);
@@ -475,6 +477,26 @@ __global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs
   }
   cooperative_groups::this_cluster().sync();   // all CTAs of the request have read its length
   if (part == 0 && threadIdx.x == 0) a.seq_len_out[b] = seq < 0 ? seq : seq + 1 + n;
+}
+
+// Clusters of sixteen CTAs are more than every device has to have: a partition of one may have none.
+cudaError_t cache_setup(ts_ctx* ctx) {
+  ctx->large_clusters = true;
+  for (void (*kernel)(const CommitArgs) : {commit_kernel<128>, commit_kernel<64>}) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(COM_LARGE); cfg.blockDim = dim3(COM_THREADS);
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = COM_LARGE; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr; cfg.numAttrs = 1;
+    int fit = 0;
+    e = cudaOccupancyMaxActiveClusters(&fit, kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    if (fit < 1) ctx->large_clusters = false;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace ts
@@ -563,10 +585,12 @@ extern "C" int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* lay, int3
   {
     ProfScope ps(ctx, K_COMMIT, st);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(B * COM_CLUSTER); cfg.blockDim = dim3(std::min(COM_THREADS, (layers * lay->Hkv + COM_CLUSTER - 1) / COM_CLUSTER * 32)); cfg.stream = st;
+    const int items = layers * lay->Hkv;
+    a.cluster = items > COM_CLUSTER * (COM_THREADS / 32) && ctx->large_clusters ? COM_LARGE : COM_CLUSTER;
+    cfg.gridDim = dim3(B * a.cluster); cfg.blockDim = dim3(std::min(COM_THREADS, (items + a.cluster - 1) / a.cluster * 32)); cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = COM_CLUSTER; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = a.cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization; attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 2;
     e = cudaLaunchKernelEx(&cfg, lay->Dh == 128 ? commit_kernel<128> : commit_kernel<64>, a);

@@ -88,6 +88,7 @@ struct ts_ctx {
   const void* tmapU_ptr; int tmapU_B;
   int tma_state;   // 0 not tried yet, 1 encoder found, -1 unavailable
   int walk_unchained;   // 1: the driver refuses a cooperative launch with programmatic serialization
+  bool large_clusters;  // the device has clusters of sixteen CTAs (ts_cache_commit)
   int tree_unchained;   // the same for the one-launch expansion
   unsigned ablation;   // TS_ABLATE_* switches (0 = the method)
   unsigned test_mode;  // TS_TEST_* switches (0 = the product's kernel selection and wait limits)

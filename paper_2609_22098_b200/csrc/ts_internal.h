@@ -18,6 +18,7 @@ cudaError_t verify_setup(ts_ctx* ctx);
 cudaError_t expand_setup(ts_ctx* ctx);
 cudaError_t walk_setup(ts_ctx* ctx);
 cudaError_t attn_setup(ts_ctx* ctx);
+cudaError_t cache_setup(ts_ctx* ctx);
 size_t level_smem_bytes(const ts_config& c);
 
 struct ScoreArgs {

@@ -414,7 +414,7 @@ def test_long_contexts_and_large_batches(dtype, Hq, Hkv, Dh, ps, lens, N, n_node
 
 
 # ------------------------------------------------------------------------------------------------ commit
-@pytest.mark.parametrize("B,layers,Hkv,Dh,ps,D,N,in_place", [(1, 1, 1, 128, 16, 4, 16, True), (5, 3, 2, 64, 16, 16, 40, False), (9, 37, 8, 128, 32, 8, 64, True), (3, 2, 3, 64, 80, 1, 1, False)])
+@pytest.mark.parametrize("B,layers,Hkv,Dh,ps,D,N,in_place", [(1, 1, 1, 128, 16, 4, 16, True), (5, 3, 2, 64, 16, 16, 40, False), (9, 37, 8, 128, 32, 8, 64, True), (3, 2, 3, 64, 80, 1, 1, False), (2, 70, 8, 64, 16, 4, 16, True)])
 def test_commit_moves_the_oracles_bytes(B, layers, Hkv, Dh, ps, D, N, in_place):
     """Paths with nodes in place, nodes that lie in other targets, the longest and the empty path, and nodes that are none."""
     rng = np.random.default_rng(B)
