@@ -508,7 +508,7 @@ void attn_place(AttnArgs& a, int QT, char* ws) {
 }
 
 // Query rows of a unit and CTAs of a launch.  Two tiles of eight rows share the unpacked keys and values, one tile leaves room for
-// three CTAs an SM (32 requests of 500 to 8,000 tokens, one tile and two: 9 rows 145 and 99 us, 16 rows 143 and 109; 8 rows need
+// three CTAs an SM (32 requests of 500 to 8,000 tokens, one tile and two: 9 rows 94 and 77 us, 16 rows 97 and 85; 8 rows need
 // only one; fp32 with 64 channels, 32 rows behind two contexts of up to 131,000 tokens 57 and 47).  fp32 with 128 channels takes
 // one: queries and weights of two parts each do not fit twice without spilling (16 requests of up to 4,000 tokens 26 and 30 us).
 static int few_tiles_of(const CacheDims& d, int rcap, bool f32) { return (long long)rcap * d.G > 8 && !(f32 && d.Dh == 128) ? 2 : 1; }
@@ -557,7 +557,7 @@ static cudaError_t attn_few_launch(ts_ctx* ctx, AttnArgs a, bool f32, char* ws, 
 }
 
 // Which kernel: tiles of 16 rows read the keys and values again for every tile, tiles of 128 pay for rows that are not there (32
-// requests of 500 to 8,000 tokens, few and many: 16 rows 109 and 150 us, 17 rows 178 and 154, 32 rows 198 and 160).
+// requests of 500 to 8,000 tokens, few and many: 16 rows 85 and 114 us, 17 rows 144 and 115, 32 rows 157 and 116).
 static bool takes_many(const CacheDims& d, int rcap, bool f32) { return !f32 && (long long)rcap * d.G > 16; }
 
 }  // namespace ts

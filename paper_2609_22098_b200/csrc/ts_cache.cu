@@ -43,15 +43,15 @@ bool on_ctx_device(const ts_ctx* ctx) {
 // requests, one warp each (and all of its warps for the many entries of a request that starts).  Small calls are one launch of a
 // cluster of eight CTAs whose barrier separates reading the counts from writing them, so that they may be updated in place;
 // where whole tables are written, many CTAs write them and a second launch updates the counts.  Bound by latency (counts, a scan, entries,
-// slots and two barriers one after the other): a round of 32 requests moves 9 KB in 7.6 us, 500 requests that start with tables of
-// up to 1,875 entries move 3.8 MB in 17.6.
+// slots and two barriers one after the other): a round of 32 requests moves 9 KB in 5.4 us, 500 requests that start with tables of
+// up to 1,875 entries move 3.8 MB in 9.7.
 // ------------------------------------------------------------------------------------------------
 constexpr int RES_THREADS = 512;
 constexpr int RES_CLUSTER = 8;
 constexpr int RES_MAX_B = 4096;
 // The cluster's form: up to this many requests and table entries (requests times columns, what the host knows).  A round of 32
-// requests with 500 columns takes the cluster 7.6 us and many CTAs 9.1, 32 whole tables of 500 columns 9.7 and 9.4, of 2,000
-// columns 11.7 and 10.3, 128 of 500 columns 20 and 10, 500 of 1,875 columns 94 and 18.
+// requests with 500 columns takes the cluster 5.2 us and many CTAs 6.4 (and the host a second launch), 32 whole tables of 500
+// columns 7.1 and 6.6, of 2,000 columns 8.9 and 7.5, 128 of 500 columns 15 and 6.8, 500 of 1,875 columns 77 and 10.
 constexpr int RES_CLUSTER_B = 64;
 constexpr long long RES_CLUSTER_ENTRIES = 1 << 16;
 
@@ -264,7 +264,7 @@ static cudaError_t launch_reserve(ts_ctx* ctx, const ReserveArgs& a, cudaStream_
 // ------------------------------------------------------------------------------------------------
 // Append.  A lane takes eight elements of a row's head (two lanes share a scale), Dh/4 lanes both K and V of one (row, head),
 // so that what is not finite in either marks both.  Chunks of 64 requests (102 to 257 rows each, 4 heads of 64 channels, fp32, with
-// values): 16.7 us for 50 MB, 3 TB/s; the trees of 32 requests in bf16 9 us for 11 MB.  Bound by issue and by the ramp of so
+// values): 12.6 us on the device for 50 MB, 4 TB/s; the trees of 32 requests in bf16 6.8 us for 11 MB.  Bound by issue and by the ramp of so
 // short a kernel; two rows a lane, side by side, took as long.
 // ------------------------------------------------------------------------------------------------
 constexpr int APP_THREADS = 128;   // (128, 256, 512: the chunks below take 12.8, 13.1, 14.5 us in a row)
