@@ -519,17 +519,17 @@ __device__ __forceinline__ void mask_scores(uint32_t (&x)[32], uint32_t on) {
 // 32 scores to fp16 weights: two a fused multiply-add and an addition (f32x2).
 __device__ __forceinline__ void weigh(const uint32_t (&x)[32], SoftRow& row, uint32_t (&w)[16]) {
   const uint64_t f2 = pair(row.f, row.f), r2 = pair(-row.ref, -row.ref);
-  uint64_t l2[2] = {pair(row.l, 0.f), pair(0.f, 0.f)};
+  uint64_t l2 = pair(row.l, 0.f);
 #pragma unroll
   for (int k = 0; k < 32; k += 2) {
     float e0, e1;
     unpair(fma2(pair(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, r2), e0, e1);
     e0 = ex2(e0); e1 = ex2(e1);
-    l2[k / 2 & 1] = add2(l2[k / 2 & 1], pair(e0, e1));
+    l2 = add2(l2, pair(e0, e1));
     w[k / 2] = as_u32(__floats2half2_rn(e0, e1));
   }
   float l0, l1;
-  unpair(add2(l2[0], l2[1]), l0, l1);
+  unpair(l2, l0, l1);
   row.l = l0 + l1;
 }
 
