@@ -343,7 +343,9 @@ int32_t ts_calib_load_table(ts_ctx* ctx, const float* table, void* stream);
  * The cache in which the target keeps its keys and values, in 4 bits, and the calls around it.  (The paper's engine keeps a
  * row of a preallocated buffer per request and a valid set, Section 4; the layout below is this library's own.)  A round of a
  * caller that uses it: ts_cache_reserve, per layer ts_cache_append and ts_tree_attention, after ts_verify_tree
- * ts_cache_commit.
+ * ts_cache_commit_granted with the reservation's status.  A request that ts_cache_reserve refused has no slots: its rows are not
+ * appended, its attention reads whatever lies there (within the pool) and means nothing, and neither does its verification
+ * (leave it out of tokens and calibration); its length stays, and the next round may serve it.
  *
  * Tokens of a request stand in pages; row b of the block table [B][max_pages] holds the page of tokens 0..page_size-1, of the
  * next page_size tokens, and so on.  seq_len[b] tokens are committed (the prefix); a round's rows are the anchor and the
@@ -422,11 +424,18 @@ int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B,
  * (pool of layer l = pool + l * layer_stride bytes); all sources of a request are read before its targets are written.
  * seq_len_out[b] = seq_len[b] + 1 + acc_len[b] (the anchor's row is in its place; may be seq_len itself); the bonus token is
  * the next round's anchor.  acc_len [B], acc_node [B][D] as written by ts_verify_tree.  Moves whose node lies outside
- * 0..Nmax-1 or whose slot has no page are skipped.  Pages stay held.  seq_len[b] < 0: nothing happens.
+ * 0..Nmax-1 or whose slot has no page are skipped.  Pages stay held.  seq_len[b] < 0: nothing happens (seq_len_out[b] =
+ * seq_len[b]).
+ *   ts_cache_commit_granted: the same with status DEVICE [B]: where it is not TS_OK nothing happens to the request.  Given the
+ *   status of ts_cache_reserve, a request that was refused pages keeps its length; ts_cache_commit, which is not told, would count
+ *   rows that were never written, and is for rounds in which no request was refused.
  */
 int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B, int32_t layers, size_t layer_stride, void* pool,
                         const int32_t* block_table, const int32_t* seq_len, const int32_t* acc_len, const int32_t* acc_node,
                         int32_t* seq_len_out, void* stream);
+int32_t ts_cache_commit_granted(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B, int32_t layers, size_t layer_stride, void* pool,
+                                const int32_t* block_table, const int32_t* seq_len, const int32_t* status, const int32_t* acc_len,
+                                const int32_t* acc_node, int32_t* seq_len_out, void* stream);
 
 /*
  * Instrumentation (no counterpart in the paper): per-kernel device times and launch counts.

@@ -27,7 +27,7 @@ EXPORTS = ("ts_create", "ts_destroy", "ts_set_ablation", "ts_set_test_mode", "ts
            "ts_score_parents", "ts_score_parents_static", "ts_expand_tree", "ts_verify_tree",
            "ts_allocate_budget", "ts_calib_accumulate", "ts_calib_refit", "ts_calib_load_table",
            "ts_emit_attention_inputs", "ts_cache_bytes", "ts_cache_reserve", "ts_cache_append",
-           "ts_tree_attention_workspace_bytes", "ts_tree_attention", "ts_cache_commit",
+           "ts_tree_attention_workspace_bytes", "ts_tree_attention", "ts_cache_commit", "ts_cache_commit_granted",
            "ts_profile_enable", "ts_profile_read", "ts_kernel_name")
 
 
@@ -81,6 +81,7 @@ def load_library() -> C.CDLL:
         L.ts_cache_append.argtypes = [vp, lay, i32, vp, i64, vp, i64] + [vp] * 4 + [vp]
         L.ts_tree_attention.argtypes = [vp, lay, i32, vp, i64] + [vp] * 5 + [f32, vp, i64, vp, vp, sz, vp]
         L.ts_cache_commit.argtypes = [vp, lay, i32, i32, sz] + [vp] * 6 + [vp]
+        L.ts_cache_commit_granted.argtypes = [vp, lay, i32, i32, sz] + [vp] * 7 + [vp]
         L.ts_profile_enable.argtypes = [vp, i32]
         L.ts_profile_read.argtypes = [vp, i32, vp, vp, i32]
         L.ts_kernel_name.argtypes = [i32]
@@ -88,7 +89,7 @@ def load_library() -> C.CDLL:
         for n in ("ts_create", "ts_destroy", "ts_score_parents", "ts_score_parents_static", "ts_expand_tree", "ts_verify_tree",
                   "ts_allocate_budget", "ts_calib_accumulate", "ts_calib_refit", "ts_calib_load_table",
                   "ts_emit_attention_inputs", "ts_cache_reserve", "ts_cache_append", "ts_tree_attention", "ts_cache_commit",
-                  "ts_profile_enable", "ts_profile_read"):
+                  "ts_cache_commit_granted", "ts_profile_enable", "ts_profile_read"):
             getattr(L, n).restype = C.c_int32
         _lib = L
     return _lib
@@ -405,16 +406,21 @@ class TreeSpark:
                          out.data_ptr(), ldo, p_lse, p_ws, ws.numel())
         return out
 
-    def cache_commit(self, lay, pool, block_table, seq_len, acc_len, acc_node, seq_len_out=None):
+    def cache_commit(self, lay, pool, block_table, seq_len, acc_len, acc_node, seq_len_out=None, status=None):
         """Move the accepted paths' rows to the ends of the prefixes, in all layers of ``pool`` ([layers, ...] or one layer);
-        returns the new lengths (in place without ``seq_len_out``)."""
+        returns the new lengths (in place without ``seq_len_out``).  ``status``: ``cache_reserve``'s; a request that it refused
+        keeps its length.  Without it no request may have been refused."""
         B = seq_len.shape[0]
         seq_len_out = seq_len if seq_len_out is None else seq_len_out
         layers = pool.shape[0] if pool.dim() == 5 else 1
         shape = (layers, *lay._pool_shape) if pool.dim() == 5 else lay._pool_shape
-        at = _check(self._index(), "cache_commit", (pool, shape, torch.uint8, "pool"), (block_table, (B, lay.max_pages), _I32, "block_table"), (seq_len, (B,), _I32, "seq_len"),
-                    (acc_len, (B,), _I32, "acc_len"), (acc_node, (B, self.D), _I32, "acc_node"), (seq_len_out, (B,), _I32, "seq_len_out"))
-        self._cache_call(self.lib.ts_cache_commit, lay.ref, B, layers, lay.layer_bytes, *at)
+        p_pool, p_table, p_len, p_status, *rest = _check(
+            self._index(), "cache_commit", (pool, shape, torch.uint8, "pool"), (block_table, (B, lay.max_pages), _I32, "block_table"), (seq_len, (B,), _I32, "seq_len"),
+            (status, (B,), _I32, "status"), (acc_len, (B,), _I32, "acc_len"), (acc_node, (B, self.D), _I32, "acc_node"), (seq_len_out, (B,), _I32, "seq_len_out"))
+        if status is None:
+            self._cache_call(self.lib.ts_cache_commit, lay.ref, B, layers, lay.layer_bytes, p_pool, p_table, p_len, *rest)
+        else:
+            self._cache_call(self.lib.ts_cache_commit_granted, lay.ref, B, layers, lay.layer_bytes, p_pool, p_table, p_len, p_status, *rest)
         return seq_len_out
 
     def verify_tree(self, U, A, W, Z, z_row_off, anchor_tok, tree, T, seed, out=None, edge_stat=True):

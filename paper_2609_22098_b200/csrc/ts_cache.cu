@@ -410,7 +410,7 @@ struct CommitArgs {
   int B, D, N, layers, cluster;
   size_t layer_stride;
   unsigned char* pool;
-  const int *table, *seq_len, *acc_len, *acc_node;
+  const int *table, *seq_len, *status, *acc_len, *acc_node;   // status may be NULL
   int* seq_len_out;
 };
 
@@ -423,7 +423,9 @@ __global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs
   pdl_launch_dependents();
   const int b = blockIdx.x / a.cluster, part = blockIdx.x - b * a.cluster;
   const int lane = threadIdx.x & 31;
-  const int seq = a.seq_len[b], n = seq < 0 ? 0 : min(max(a.acc_len[b], 0), a.D);
+  const int seq = a.seq_len[b];
+  const bool idle = seq < 0 || (a.status && a.status[b] != TS_OK);   // (no rows of this round: one that was refused pages wrote none)
+  const int n = idle ? 0 : min(max(a.acc_len[b], 0), a.D);
   if (threadIdx.x < DMAX) {
     const int i = threadIdx.x;
     long long f = -1, t = -1;
@@ -476,7 +478,7 @@ __global__ void __launch_bounds__(COM_THREADS, 1) commit_kernel(const CommitArgs
     __syncwarp();
   }
   cooperative_groups::this_cluster().sync();   // all CTAs of the request have read its length
-  if (part == 0 && threadIdx.x == 0) a.seq_len_out[b] = seq < 0 ? seq : seq + 1 + n;
+  if (part == 0 && threadIdx.x == 0) a.seq_len_out[b] = idle ? seq : seq + 1 + n;
 }
 
 // Clusters of sixteen CTAs are more than every device has to have: a partition of one may have none.
@@ -563,23 +565,28 @@ extern "C" int32_t ts_cache_append(ts_ctx* ctx, const ts_cache_layout* lay, int3
   return e == cudaSuccess ? TS_OK : set_cuda_error("ts_cache_append", e);
 }
 
-extern "C" int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* lay, int32_t B, int32_t layers, size_t layer_stride, void* pool,
-                                   const int32_t* block_table, const int32_t* seq_len, const int32_t* acc_len, const int32_t* acc_node,
-                                   int32_t* seq_len_out, void* stream) {
-  if (!ctx) return set_error(TS_ERR_INVALID, "ts_cache_commit: null context");
-  if (cache_layout_error(lay)) return set_layout_error("ts_cache_commit", lay);
-  if (bad_ptr(pool)) return set_error(TS_ERR_INVALID, "ts_cache_commit: null or misaligned pointer");
+static int32_t commit_paths(const char* call, ts_ctx* ctx, const ts_cache_layout* lay, int32_t B, int32_t layers, size_t layer_stride, void* pool,
+                            const int32_t* block_table, const int32_t* seq_len, const int32_t* status, const int32_t* acc_len, const int32_t* acc_node,
+                            int32_t* seq_len_out, void* stream) {
+  auto refuse = [call](const char* why) {
+    char msg[160];
+    snprintf(msg, sizeof(msg), "%s: %s", call, why);
+    return set_error(TS_ERR_INVALID, msg);
+  };
+  if (!ctx) return refuse("null context");
+  if (cache_layout_error(lay)) return set_layout_error(call, lay);
+  if (bad_ptr(pool)) return refuse("null or misaligned pointer");
   const void* req[] = {block_table, seq_len, acc_len, acc_node, seq_len_out};
   for (const void* p : req)
-    if (bad_ptr4(p)) return set_error(TS_ERR_INVALID, "ts_cache_commit: null or misaligned pointer");
-  if (B < 1 || B > ctx->cfg.max_batch) return set_error(TS_ERR_INVALID, "ts_cache_commit: B out of range");
-  if (layers < 1 || layers > 4096) return set_error(TS_ERR_INVALID, "ts_cache_commit: layers out of range");
-  if (layers > 1 && (layer_stride < ts_cache_bytes(lay) || layer_stride % 16)) return set_error(TS_ERR_INVALID, "ts_cache_commit: layer stride must cover a layer's pool and be a multiple of 16 bytes");
-  if (!on_ctx_device(ctx)) return set_error(TS_ERR_INVALID, "ts_cache_commit: the context's device is not the current one");
+    if (bad_ptr4(p)) return refuse("null or misaligned pointer");
+  if (B < 1 || B > ctx->cfg.max_batch) return refuse("B out of range");
+  if (layers < 1 || layers > 4096) return refuse("layers out of range");
+  if (layers > 1 && (layer_stride < ts_cache_bytes(lay) || layer_stride % 16)) return refuse("layer stride must cover a layer's pool and be a multiple of 16 bytes");
+  if (!on_ctx_device(ctx)) return refuse("the context's device is not the current one");
   CommitArgs a{};
   a.d = cache_dims(lay);
   a.B = B; a.D = ctx->cfg.D; a.N = ctx->cfg.Nmax; a.layers = layers; a.layer_stride = layer_stride; a.pool = (unsigned char*)pool;
-  a.table = block_table; a.seq_len = seq_len; a.acc_len = acc_len; a.acc_node = acc_node; a.seq_len_out = seq_len_out;
+  a.table = block_table; a.seq_len = seq_len; a.status = status; a.acc_len = acc_len; a.acc_node = acc_node; a.seq_len_out = seq_len_out;
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e;
   {
@@ -596,5 +603,18 @@ extern "C" int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* lay, int3
     e = cudaLaunchKernelEx(&cfg, lay->Dh == 128 ? commit_kernel<128> : commit_kernel<64>, a);
   }
   if (e == cudaSuccess) e = cudaGetLastError();
-  return e == cudaSuccess ? TS_OK : set_cuda_error("ts_cache_commit", e);
+  return e == cudaSuccess ? TS_OK : set_cuda_error(call, e);
+}
+
+extern "C" int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* lay, int32_t B, int32_t layers, size_t layer_stride, void* pool,
+                                   const int32_t* block_table, const int32_t* seq_len, const int32_t* acc_len, const int32_t* acc_node,
+                                   int32_t* seq_len_out, void* stream) {
+  return commit_paths("ts_cache_commit", ctx, lay, B, layers, layer_stride, pool, block_table, seq_len, nullptr, acc_len, acc_node, seq_len_out, stream);
+}
+
+extern "C" int32_t ts_cache_commit_granted(ts_ctx* ctx, const ts_cache_layout* lay, int32_t B, int32_t layers, size_t layer_stride, void* pool,
+                                           const int32_t* block_table, const int32_t* seq_len, const int32_t* status, const int32_t* acc_len,
+                                           const int32_t* acc_node, int32_t* seq_len_out, void* stream) {
+  if (bad_ptr4(status)) return set_error(TS_ERR_INVALID, "ts_cache_commit_granted: null or misaligned pointer");
+  return commit_paths("ts_cache_commit_granted", ctx, lay, B, layers, layer_stride, pool, block_table, seq_len, status, acc_len, acc_node, seq_len_out, stream);
 }

@@ -1,0 +1,21 @@
+"""Refusals and checks of the cache calls that need no device (see test_cache_refusals.py)."""
+import ctypes as C
+
+import pytest
+
+from paper_2609_22098_b200 import binding
+from test_cache_refusals import OK, ctx, layout, lib   # noqa: F401 (fixtures)
+
+
+def granted(lib, ctx, lay, B=2, layers=3, ptrs=None):
+    return lib.ts_cache_commit_granted(ctx, C.byref(lay), B, layers, lib.ts_cache_bytes(C.byref(lay)), *(ptrs or [OK] * 7), None)
+
+
+def test_commit_with_status_checks_what_commit_checks(lib, ctx):
+    for bad in (None, OK + 2):
+        for i in range(7):
+            assert granted(lib, ctx, layout(), ptrs=[bad if j == i else OK for j in range(7)]) == -1, i
+            assert lib.ts_last_error_string().startswith(b"ts_cache_commit_granted: ")
+    assert granted(lib, None, layout()) == -1 and granted(lib, ctx, layout(), B=9) == -1 and granted(lib, ctx, layout(), layers=0) == -1
+    assert granted(lib, ctx, layout(Dh=96)) == -2 and lib.ts_last_error_string().startswith(b"ts_cache_commit_granted: head size")
+    assert granted(lib, ctx, layout()) == -1 and lib.ts_last_error_string() == b"ts_cache_commit_granted: the context's device is not the current one"
