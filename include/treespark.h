@@ -376,8 +376,8 @@ size_t ts_cache_bytes(const ts_cache_layout* layout);
  * free_pages[free_count - 1 - k].  New table entries held[b] .. are written, others are left as they are.  A request whose
  * pages would pass the list's beginning, or that needs more than max_pages, is refused: status TS_ERR_OVERFLOW, no slots,
  * nothing taken; so are all later ones that need pages (those that need none are served).
- * seq_len[b] < 0: the request's pages go back to the list, its table entries become -1, held 0.  They can be taken by the
- * next call.
+ * seq_len[b] < 0: the request's pages go back to the list (entries that are no page are dropped), its table entries become -1, held 0.
+ * They can be taken by the next call.  The free_count entries of the list have to be pages of the pool, each once and in no table.
  *   slot_map [B][Nmax+1] ([B][1]): slot of each row, -1 for unused rows, refused requests and entries that are no page.
  *   held_out [B], free_count_out [1]: the new counts; may be the arrays held and free_count themselves.
  *   status [B]: TS_OK or TS_ERR_OVERFLOW.

@@ -117,7 +117,7 @@ def reserve(page_size, n_pages, seq_len, rows, held, free_pages, free_count, tab
     count, status, slots, back, short = int(free_count), [0] * B, np.full((B, R), -1, np.int64), [], False
     for b in range(B):
         if seq_len[b] < 0:
-            back += [int(p) for p in table[b, :held[b]]]
+            back += [int(p) for p in table[b, :held[b]] if 0 <= p < n_pages]   # (other entries are no pages)
             table[b, :held[b]] = -1
             held[b] = 0
             continue

@@ -78,7 +78,7 @@ __device__ __forceinline__ int pages_taken(const ReserveArgs& a, int b) {
   return need < 0 || need > a.d.cols ? 0 : max(0, need - pages_held(a, b));
 }
 
-// pages taken (low half) and given back (high half); each half stops at 2^31 - 1, which is more than a pool has pages
+// pages taken (low half) and entries given back (high half); each half stops at 2^31 - 1, which is more than a pool has pages
 __device__ __forceinline__ long long pages_of(const ReserveArgs& a, int b) {
   return (long long)pages_taken(a, b) + (a.seq_len[b] < 0 ? (long long)pages_held(a, b) << 32 : 0ll);
 }
@@ -87,12 +87,13 @@ __device__ __forceinline__ long long add_pages(long long x, long long y) {
   return (long long)((unsigned long long)min((unsigned)(x >> 32) + (unsigned)(y >> 32), top) << 32 | min((unsigned)x + (unsigned)y, top));
 }
 
-// Exclusive running sums over requests, in shared memory; returns the total.
-__device__ long long reserve_scan(const ReserveArgs& a, long long* pre) {
+// Exclusive running sums over requests of what `of` says, in shared memory (where `of` may look for its own request); returns the total.
+template <class Of>
+__device__ long long reserve_scan(int B, long long* pre, Of of) {
   __shared__ long long wsum[RES_THREADS / 32];
-  const int per = (a.B + RES_THREADS - 1) / RES_THREADS, b0 = threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = (B + RES_THREADS - 1) / RES_THREADS, b0 = threadIdx.x * per, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   long long sum = 0;
-  for (int b = b0; b < min(b0 + per, a.B); ++b) sum = add_pages(sum, pre[b] = pages_of(a, b));
+  for (int b = b0; b < min(b0 + per, B); ++b) sum = add_pages(sum, pre[b] = of(b));
   long long inc = sum;
   for (int o = 1; o < 32; o <<= 1) {
     const long long v = __shfl_up_sync(~0u, inc, o);
@@ -107,7 +108,7 @@ __device__ long long reserve_scan(const ReserveArgs& a, long long* pre) {
     if (w < warp) at = add_pages(wsum[w], at);
     all = add_pages(all, wsum[w]);
   }
-  for (int b = b0; b < min(b0 + per, a.B); ++b) {
+  for (int b = b0; b < min(b0 + per, B); ++b) {
     const long long mine = pre[b];
     pre[b] = at;
     at = add_pages(at, mine);
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
   const int count = min(max(a.free_count[0], 0), a.d.n_pages);
-  const long long all = reserve_scan(a, pre);
+  const long long all = reserve_scan(a.B, pre, [&](int b) { return pages_of(a, b); });
   if (WHERE == 2 || WHERE == 0) {
     const int taken = reserve_taken(a, pre, count);
     // the plans of this thread's requests, before anything is written in place
@@ -203,20 +204,45 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
         new_held[k] = p.release ? 0 : p.granted ? max(p.held, p.need) : p.held;
       }
     }
+    // Entries that are pages, of the requests that give theirs back: what else stands in a table does not go on the list.  (Every CTA
+    // counts all of them, and before any of them is overwritten.)
+    const bool gives = all >> 32 != 0;   // (the same in all CTAs)
+    long long back = 0;
+    if (gives) {
+      __syncthreads();   // the sums of taken pages are not needed any more
+      for (int b = threadIdx.x >> 5; b < a.B; b += RES_THREADS / 32) {
+        int n = 0;
+        if (a.seq_len[b] < 0) {
+          const int held = pages_held(a, b);
+          const int* row = a.table + (size_t)b * a.d.cols;
+#pragma unroll 4
+          for (int c = lane; c < held; c += 32) n += (unsigned)row[c] < (unsigned)a.d.n_pages;
+        }
+        n = __reduce_add_sync(~0u, n);
+        if (lane == 0) pre[b] = n;
+      }
+      __syncthreads();
+      back = reserve_scan(a.B, pre, [&](int b) { return pre[b]; });
+    }
     // Given-back pages go where the taken ones lay: every CTA has read those by now.
     const int base = count - taken;
     if (WHERE == 0) cooperative_groups::this_cluster().sync();
     else __syncthreads();
-    const bool gives = all >> 32 != 0;   // (the same in all CTAs)
     for (int b = me; gives && b < a.B; b += warps) {
       if (a.seq_len[b] >= 0) continue;
       // (held[b] may be written by CTA 0 below once all have passed the second barrier only)
-      const int n = pages_held(a, b), at = base + (int)(pre[b] >> 32);
+      const int n = pages_held(a, b);
+      long long at = base + pre[b];   // (in 64 bits: a table may name a page twice)
       int* row = a.table + (size_t)b * a.d.cols;
-      for (int c = lane; c < n; c += 32) {
-        const int page = row[c];
-        row[c] = -1;
-        if (at + c < a.d.n_pages) a.free_pages[at + c] = page;
+#pragma unroll 4
+      for (int c0 = 0; c0 < n; c0 += 32) {
+        const int c = c0 + lane, page = c < n ? row[c] : -1;
+        const bool is_page = (unsigned)page < (unsigned)a.d.n_pages;
+        const unsigned are = __ballot_sync(~0u, is_page);
+        const long long to = at + __popc(are & ((1u << lane) - 1u));
+        if (c < n) row[c] = -1;
+        if (is_page && to < a.d.n_pages) a.free_pages[to] = page;
+        at += __popc(are);
       }
     }
     if (gives) {
@@ -230,7 +256,7 @@ __global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs 
         if (b >= a.B) break;
         a.held_out[b] = new_held[k];
       }
-      if (threadIdx.x == 0) a.free_count_out[0] = min(base + (int)(all >> 32), a.d.n_pages);
+      if (threadIdx.x == 0) a.free_count_out[0] = (int)min(base + back, (long long)a.d.n_pages);
     }
   } else {
     reserve_tables(a, pre, count);

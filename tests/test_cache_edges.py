@@ -1,8 +1,10 @@
 """Refusals and checks of the cache calls that need no device (see test_cache_refusals.py)."""
 import ctypes as C
 
+import numpy as np
 import pytest
 
+from oracle import cache as oc
 from paper_2609_22098_b200 import binding
 from test_cache_refusals import OK, ctx, layout, lib   # noqa: F401 (fixtures)
 
@@ -19,3 +21,9 @@ def test_commit_with_status_checks_what_commit_checks(lib, ctx):
     assert granted(lib, None, layout()) == -1 and granted(lib, ctx, layout(), B=9) == -1 and granted(lib, ctx, layout(), layers=0) == -1
     assert granted(lib, ctx, layout(Dh=96)) == -2 and lib.ts_last_error_string().startswith(b"ts_cache_commit_granted: head size")
     assert granted(lib, ctx, layout()) == -1 and lib.ts_last_error_string() == b"ts_cache_commit_granted: the context's device is not the current one"
+
+
+def test_oracle_gives_back_pages_only():
+    table = np.array([[3, -1, 99, 5], [0, 1, -1, -1]])
+    t, held, free, count, _, status = oc.reserve(16, 8, [-1, 20], [1, 1], [4, 2], [7, 2, 4, 6, 0, 0, 0, 0], 4, table, 1)
+    assert t.tolist() == [[-1] * 4, [0, 1, -1, -1]] and held == [0, 2] and free[:count] == [7, 2, 4, 6, 3, 5] and status == [0, 0]

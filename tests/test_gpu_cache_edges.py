@@ -9,9 +9,40 @@ import torch
 from oracle import cache as oc
 from paper_2609_22098_b200 import synth
 from paper_2609_22098_b200.binding import CacheLayout, TreeSpark
-from test_gpu_cache import BF16, F32, context, i32, random_table, round_inputs
+from test_gpu_cache import BF16, check_reserve, context, i32, random_table, round_inputs
 
 pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ reserve
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,cols,pages,seed", [(1, 4, 8, 0), (6, 70, 300, 1), (64, 300, 9000, 2), (3, 30000, 50000, 3), (300, 90, 20000, 4), (4096, 5, 9000, 5)])
+def test_pages_given_back_are_pages(B, cols, pages, seed, in_place):
+    """Tables with entries that are no pages (negative, the pool's end, far beyond) at any place: released, they are dropped, and the
+    list holds each page once.  One cluster and many CTAs."""
+    rng = np.random.default_rng(seed)
+    ts, lay = context(4, B), CacheLayout(4, 2, 64, 16, pages, cols)
+    held = rng.integers(0, cols + 1, B)
+    held = np.minimum(held, pages // B)
+    order, at = rng.permutation(pages), 0
+    table = np.full((B, cols), -1, np.int64)
+    for b in range(B):
+        table[b, :held[b]] = order[at:at + held[b]]
+        at += held[b]
+    free, count = np.zeros(pages, np.int64), pages - at
+    free[:count] = order[at:]
+    own = np.arange(cols)[None] < held[:, None]
+    junk = own & (rng.random((B, cols)) < 0.2)
+    junk[0, :held[0]] |= seed == 0      # one request without a single page
+    table[junk] = rng.choice([-1, -7, pages, pages + 1, 1 << 30], int(junk.sum()))
+    seq = np.where(rng.random(B) < 0.6, -1, rng.integers(0, 16 * cols - 8, B))
+    seq[0] = -1
+    w = check_reserve(ts, lay, seq, rng.integers(0, 5, B), held.tolist(), free, count, table, in_place)
+    left = [int(p) for p in w[2][:w[3]]]
+    assert len(set(left)) == len(left) and all(0 <= p < pages for p in left)
+    check_reserve(ts, lay, [0] * B, None, w[1], w[2], w[3], w[0], in_place)
+    all_back = check_reserve(ts, lay, [-1] * B, None, w[1], w[2], w[3], w[0], in_place)
+    assert all_back[3] == pages - int(junk.sum())
 
 
 # ------------------------------------------------------------------------------------------------ commit
