@@ -409,7 +409,7 @@ int32_t ts_cache_append(ts_ctx* ctx, const ts_cache_layout* layout, int32_t rows
  * q and out: [B][Nmax+1][Hq][Dh] ([B][Hq][Dh] without n_nodes) with ldq, ldo elements between rows; the rows of this round
  * have been appended.  |scale| and |scale| * 2^k_exp are at most 1e30; scores have to fit float (a row with one beyond it is not
  * defined).  Unused rows and requests with seq_len < 0 are left as they were.  Tokens whose table entry is no
- * page are absent; a row that sees no token gets 0 and lse = -inf.  What stands in the cache behind the last row, or in
+ * page are absent; a row that sees no token gets 0 and lse = -inf, one whose query is not finite and that sees any gets NaN.  What stands in the cache behind the last row, or in
  * nodes that a row does not see, does not matter, NaN included.  ws: ts_tree_attention_workspace_bytes() bytes (it does not
  * grow with B or the lengths); calls that overlap on the GPU, replayed graphs among them, need one each.  A bounded
  * device-side wait that runs out gives NaN (bf16 with more than 16 rows a kv head; the other kernels have no such waits).

@@ -96,7 +96,9 @@ struct Queries {
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
       const int e = max((int)(__float_as_uint(top) >> 23), 20);         // biased exponent; 2^(141 - e) has to be a float
-      const float up = copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk), mine = fmaxf(1e-30f, fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23));
+      // (a row with an infinity has no finite score: it becomes NaN, so that one whose scores are all -inf is no empty row)
+      const float up = e < 255 ? copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk) : NAN;
+      const float mine = fmaxf(1e-30f, fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23));
 #pragma unroll
       for (int i = 0; i < REGS; ++i) {
         const float x0 = x[2 * i] * up, x1 = x[2 * i + 1] * up;

@@ -437,7 +437,7 @@ __device__ __forceinline__ void load_queries(const AttnArgs& a, const AttnUnit& 
       for (int x = L / 2; x; x >>= 1) top = __vmaxu2(top, __shfl_xor_sync(~0u, top, x));
       const int e = max((int)(max(top & 0xFFFFu, top >> 16) >> 7), 20);
       // (the sign of the scale goes to the queries: the largest score is the factor times the largest sum)
-      const float up = copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk);
+      const float up = e < 255 ? copysignf(__uint_as_float((unsigned)(127 + 141 - e) << 23), a.qk) : NAN;   // (not finite: NaN, see there)
       const int r = row - lane + k0 + k * R + sub;
       if (c == 0) f[r] = fabsf(a.qk) * __uint_as_float((unsigned)(127 + e - 141) << 23);
       float x[8];

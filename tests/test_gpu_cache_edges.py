@@ -9,7 +9,7 @@ import torch
 from oracle import cache as oc
 from paper_2609_22098_b200 import synth
 from paper_2609_22098_b200.binding import CacheLayout, TreeSpark
-from test_gpu_cache import BF16, check_reserve, context, i32, random_table, round_inputs
+from test_gpu_cache import BF16, F32, check_reserve, context, i32, random_table, round_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -43,6 +43,27 @@ def test_pages_given_back_are_pages(B, cols, pages, seed, in_place):
     check_reserve(ts, lay, [0] * B, None, w[1], w[2], w[3], w[0], in_place)
     all_back = check_reserve(ts, lay, [-1] * B, None, w[1], w[2], w[3], w[0], in_place)
     assert all_back[3] == pages - int(junk.sum())
+
+
+# ------------------------------------------------------------------------------------------------ attention
+@pytest.mark.parametrize("dtype,Hq,Dh", [(BF16, 1, 64), (BF16, 16, 128), (BF16, 32, 64), (BF16, 40, 128), (F32, 3, 64), (F32, 2, 128)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_queries_with_infinities_give_nan_whatever_their_scores(dtype, Hq, Dh, sign):
+    """One or more visible tokens whose keys have one sign: a query of zeros and one infinity scores +inf or -inf on all of them,
+    and with both the softmax has no value.  A row that sees nothing stays 0."""
+    ts, lay = context(dtype=dtype, Nmax=4), CacheLayout(Hq, 1, Dh, 16, 40, 33, dtype)
+    pool = torch.zeros(lay.pool_shape(), dtype=torch.uint8, device="cuda")
+    k = torch.ones(33 * 16, 1, Dh, dtype=dtype, device="cuda")
+    ts.cache_append(lay, k, k, i32(range(33 * 16)), pool)
+    q = torch.zeros(3, Hq, Dh, dtype=dtype, device="cuda")
+    q[:, ::2, 5] = sign * float("inf")
+    q[:, 1::2] = 1.0
+    table = np.stack([np.arange(33), np.arange(33), np.full(33, -1)])
+    lse = torch.full((3, Hq), -5.0, device="cuda")
+    out = ts.tree_attention(lay, q, pool, i32(table), i32([0, 520, 7]), lse=lse)
+    assert torch.isnan(out[:2, ::2]).all() and torch.isnan(lse[:2, ::2]).all()
+    assert torch.isfinite(out[:2, 1::2]).all() and torch.isfinite(lse[:2, 1::2]).all()
+    assert not out[2].any() and torch.isneginf(lse[2]).all()
 
 
 # ------------------------------------------------------------------------------------------------ commit
