@@ -51,6 +51,7 @@ struct ManyBars {
   uint64_t raw_full[MANY_RAW], raw_free[MANY_RAW];
   uint64_t k_full[2], v_full[2], k_free[2][2], v_free[2][2];   // (free: by group and stage)
   uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+  uint64_t issued;   // all products
 };
 
 __device__ __forceinline__ void mma_tmem_a(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -133,6 +134,11 @@ __device__ __forceinline__ ManySegment many_segment(const AttnArgs& a, const Att
   return s;
 }
 
+// A bounded wait that other waits' giving up does not end.
+__device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity, uint32_t limit) {
+  for (uint32_t i = 0; i < limit && !mbar_try_wait(bar, parity); ++i) __nanosleep(100);
+}
+
 // ---- loader -------------------------------------------------------------------------------------------------------------
 // The warp's lanes have a block each of four steps: looked up in the table together, asked for in L2 at once, and copied one
 // batch later, half a step at a time.  (The ring alone has room for 27 KB on their way, less than memory needs; and one look-up
@@ -175,7 +181,7 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
       if (lane == 0) {
         unsigned char* pr = &sh.present[(copied >> 1) % MANY_PRESENT];
         *pr = (unsigned char)((copied & 1) ? *pr | there << 4 : there);
-        mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * BLK + a.lost);
+        mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * BLK + (copied >= min(4, half_steps - 1) ? a.lost : 0u));   // (from the third step on, or the last)
       }
       __syncwarp();
       if (lane >> 2 == k && now >= 0)
@@ -186,10 +192,9 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
     }
     now = place();
   }
-  // after a wait that gave up copies may still be on their way (the last use of a slot completes the phase before the next)
-  if (sh.abort)
-    for (int s = 0; s < MANY_RAW && s < copied; ++s)
-      for (uint32_t i = 0; i < a.limit && !mbar_try_wait(&sh.bars.raw_full[s], s < slot ? phase : phase ^ 1u); ++i) __nanosleep(100);
+  // Shared memory is not given up before the last copies have come, whichever wait gives up and when (the last use of a slot completes
+  // the phase before the next).
+  for (int s = 0; s < MANY_RAW && s < copied; ++s) drain(&sh.bars.raw_full[s], s < slot ? phase : phase ^ 1u, a.limit);
 }
 
 // ---- converters ---------------------------------------------------------------------------------------------------------
@@ -726,6 +731,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
       mbar_init(&b.v_full[s], MANY_CONV / 2); mbar_init(&b.v_free[0][s], 1); mbar_init(&b.v_free[1][s], 1);
       mbar_init(&b.q_full[s], MANY_SOFT); mbar_init(&b.s_full[s], 1); mbar_init(&b.p_full[s], MANY_SOFT / 2); mbar_init(&b.o_full[s], 1);
     }
+    mbar_init(&b.issued, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_wait();
@@ -750,7 +756,13 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
       many_convert<KeyPart<Dh>, Dh>(a, sh, smem + P::R, smem + P::K, sh.bars.k_full, sh.bars.k_free, threadIdx.x - MANY_SOFT * 32);
     else if (warp < MANY_ISSUE)
       many_convert<ValuePart<Dh>, Dh>(a, sh, smem + P::R, smem + P::V, sh.bars.v_full, sh.bars.v_free, threadIdx.x - MANY_SOFT * 32 - MANY_CT);
-    else if (warp == MANY_ISSUE) { if (elect_one()) many_issue<Dh>(a, sh, smem); }
+    else if (warp == MANY_ISSUE) {
+      if (elect_one()) {
+        many_issue<Dh>(a, sh, smem);
+        mma_commit(&sh.bars.issued);   // (nor is tensor memory before the last products are complete)
+        drain(&sh.bars.issued, 0u, a.limit);
+      }
+    }
     else if (warp == MANY_LOAD) many_load<Dh>(a, sh, smem + P::R);
   }
   tc_fence_before();

@@ -7,9 +7,9 @@ import pytest
 import torch
 
 from oracle import cache as oc
-from paper_2609_22098_b200 import synth
+from paper_2609_22098_b200 import binding, synth
 from paper_2609_22098_b200.binding import CacheLayout, TreeSpark
-from test_gpu_cache import BF16, F32, check_reserve, context, i32, random_table, round_inputs
+from test_gpu_cache import BF16, F32, check_reserve, context, i32, random_pool, random_table, round_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -64,6 +64,27 @@ def test_queries_with_infinities_give_nan_whatever_their_scores(dtype, Hq, Dh, s
     assert torch.isnan(out[:2, ::2]).all() and torch.isnan(lse[:2, ::2]).all()
     assert torch.isfinite(out[:2, 1::2]).all() and torch.isfinite(lse[:2, 1::2]).all()
     assert not out[2].any() and torch.isneginf(lse[2]).all()
+
+
+@pytest.mark.parametrize("Dh,N,Hq", [(128, 1, 32), (64, 1, 24), (128, 4, 48), (64, 7, 32)])
+def test_a_wait_that_runs_out_behind_issued_products(Dh, N, Hq):
+    """The tensor-core kernel gives up in the third of some ten steps a CTA, with products of the steps before issued: it waits for them
+    and for its copies, its rows are NaN, and the same call without lost bytes gives what it gave before."""
+    ts = context(Nmax=N, B=1)
+    n = 10 * 128 * torch.cuda.get_device_properties(0).multi_processor_count
+    pages = n // 64 + 1
+    lay = CacheLayout(Hq, 1, Dh, 64, pages, pages)
+    pool = random_pool(2, lay.pool_shape())
+    table = i32(np.random.default_rng(0).permutation(pages)[None])
+    q = torch.randn(1, N + 1, Hq, Dh, device="cuda").to(BF16)
+    args, kw = (lay, q, pool, table, i32([n])), dict(n_nodes=i32([N]))
+    good = ts.tree_attention(*args, **kw)
+    ts.set_test_mode(binding.TEST_SHORT_WAITS | binding.TEST_LOST_ARRIVAL)
+    lse = torch.zeros(1, N + 1, Hq, device="cuda")
+    lost = ts.tree_attention(*args, **kw, lse=lse)
+    assert torch.isnan(lost).all() and torch.isnan(lse).all()
+    ts.set_test_mode(0)
+    assert torch.isfinite(good).all() and torch.equal(ts.tree_attention(*args, **kw), good)
 
 
 # ------------------------------------------------------------------------------------------------ commit
