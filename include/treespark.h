@@ -375,8 +375,9 @@ size_t ts_cache_bytes(const ts_cache_layout* layout);
  * Pages and slots for a round.  Request b needs ceil((seq_len + rows) / page_size) pages and has held[b]; what is missing is
  * taken from the end of free_pages [n_pages] (free_count[0] entries), the first request first: the k-th page taken is
  * free_pages[free_count - 1 - k].  New table entries held[b] .. are written, others are left as they are.  A request whose
- * pages would pass the list's beginning, or that needs more than max_pages, is refused: status TS_ERR_OVERFLOW, no slots,
- * nothing taken; so are all later ones that need pages (those that need none are served).
+ * pages would pass the list's beginning is refused: status TS_ERR_OVERFLOW, no slots, nothing taken; so are all later ones that
+ * need pages (those that need none are served).  A request that needs more than max_pages is refused alone: later ones are served
+ * as if it were not there.
  * seq_len[b] < 0: the request's pages go back to the list (entries that are no page are dropped), its table entries become -1, held 0.
  * They can be taken by the next call.  The free_count entries of the list have to be pages of the pool, each once and in no table.
  *   slot_map [B][Nmax+1] ([B][1]): slot of each row, -1 for unused rows, refused requests and entries that are no page.

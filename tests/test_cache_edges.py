@@ -27,3 +27,14 @@ def test_oracle_gives_back_pages_only():
     table = np.array([[3, -1, 99, 5], [0, 1, -1, -1]])
     t, held, free, count, _, status = oc.reserve(16, 8, [-1, 20], [1, 1], [4, 2], [7, 2, 4, 6, 0, 0, 0, 0], 4, table, 1)
     assert t.tolist() == [[-1] * 4, [0, 1, -1, -1]] and held == [0, 2] and free[:count] == [7, 2, 4, 6, 3, 5] and status == [0, 0]
+
+
+def test_oracle_refuses_a_request_beyond_the_table_alone():
+    """Requests 0 to 4: one fits, one needs more pages than the table has columns, one fits, one finds the list too short, and so
+    does the next, which needs one page of the two that are left; the last needs none."""
+    table = np.full((6, 3), -1)
+    table[5, 0] = 9
+    t, held, free, count, slots, status = oc.reserve(16, 10, [3, 40, 20, 30, 0, 3], [4, 9, 4, 18, 2, 4], [0, 0, 0, 0, 0, 1], [0, 1, 2, 3, 4], 5, table, 18)
+    assert status == [0, oc.OVERFLOW, 0, oc.OVERFLOW, oc.OVERFLOW, 0]
+    assert held == [1, 0, 2, 0, 0, 1] and count == 2 and t[2].tolist() == [3, 2, -1]
+    assert (slots >= 0).sum(1).tolist() == [4, 0, 4, 0, 0, 4]

@@ -45,6 +45,17 @@ def test_pages_given_back_are_pages(B, cols, pages, seed, in_place):
     assert all_back[3] == pages - int(junk.sum())
 
 
+@pytest.mark.parametrize("B", [6, 80])
+def test_a_request_beyond_the_table_is_refused_alone(B):
+    """On the one-cluster form and on many CTAs, by the six requests of the oracle's own test (idle ones behind them)."""
+    ts, lay = context(20, B), CacheLayout(4, 2, 64, 16, 10, 3)
+    table = np.full((B, 3), -1, np.int64)
+    table[5, 0] = 9
+    idle = B - 6
+    w = check_reserve(ts, lay, [3, 40, 20, 30, 0, 3] + [-1] * idle, [3, 8, 3, 17, 1, 3] + [0] * idle, [0, 0, 0, 0, 0, 1] + [0] * idle, [0, 1, 2, 3, 4, 0, 0, 0, 0, 0], 5, table, True)
+    assert w[5][:6] == [0, -6, 0, -6, -6, 0] and w[1][:6] == [1, 0, 2, 0, 0, 1]
+
+
 # ------------------------------------------------------------------------------------------------ attention
 @pytest.mark.parametrize("dtype,Hq,Dh", [(BF16, 1, 64), (BF16, 16, 128), (BF16, 32, 64), (BF16, 40, 128), (F32, 3, 64), (F32, 2, 128)])
 @pytest.mark.parametrize("sign", [1.0, -1.0])
