@@ -133,6 +133,8 @@ def _rows_of(t: torch.Tensor, heads: int, Dh: int, dtype, index: int, what: str)
         raise TreeSparkError(f"{what}: expected {dtype} [..., {heads}, {Dh}] on device {index}, got {t.dtype} {tuple(shape)} on {t.device}")
     if stride[-1] != 1 or (heads > 1 and stride[-2] != Dh):
         raise TreeSparkError(f"{what}: the {heads} heads of a row must be contiguous")
+    if t.numel() == 0:
+        return 0, heads * Dh
     ld, rows = 0, 1
     for i in range(len(shape) - 3, -1, -1):
         n = shape[i]

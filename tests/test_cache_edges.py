@@ -3,6 +3,7 @@ import ctypes as C
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import cache as oc
 from paper_2609_22098_b200 import binding
@@ -38,3 +39,13 @@ def test_oracle_refuses_a_request_beyond_the_table_alone():
     assert status == [0, oc.OVERFLOW, 0, oc.OVERFLOW, oc.OVERFLOW, 0]
     assert held == [1, 0, 2, 0, 0, 1] and count == 2 and t[2].tolist() == [3, 2, -1]
     assert (slots >= 0).sum(1).tolist() == [4, 0, 4, 0, 0, 4]
+
+
+@pytest.mark.parametrize("shape", [(0, 2, 64), (4, 0, 2, 64), (0, 5, 2, 64), (3, 0, 7, 2, 64)])
+def test_no_rows_are_rows(shape):
+    """Tensors of no rows, whatever the other dimensions are: strides say nothing there."""
+    t = torch.zeros(shape, dtype=torch.bfloat16)
+    assert binding._rows_of(t, 2, 64, torch.bfloat16, -1, "k") == (0, 128)
+    assert binding._rows_of(torch.zeros(*shape[:-2], 6, 64, dtype=torch.bfloat16)[..., 2:4, :], 2, 64, torch.bfloat16, -1, "k") == (0, 128)
+    with pytest.raises(binding.TreeSparkError):
+        binding._rows_of(t, 3, 64, torch.bfloat16, -1, "k")

@@ -56,6 +56,15 @@ def test_a_request_beyond_the_table_is_refused_alone(B):
     assert w[5][:6] == [0, -6, 0, -6, -6, 0] and w[1][:6] == [1, 0, 2, 0, 0, 1]
 
 
+@pytest.mark.parametrize("shape", [(0,), (4, 0), (0, 5)])
+def test_append_of_no_rows(shape):
+    ts, lay = context(), CacheLayout(2, 2, 64, 16, 3, 3)
+    pool = torch.full(lay.pool_shape(), 77, dtype=torch.uint8, device="cuda")
+    k = torch.zeros(*shape, 2, 64, dtype=BF16, device="cuda")
+    ts.cache_append(lay, k, k, torch.zeros(shape, dtype=torch.int32, device="cuda"), pool, k_val=torch.empty_like(k))
+    assert (pool == 77).all()
+
+
 # ------------------------------------------------------------------------------------------------ attention
 @pytest.mark.parametrize("dtype,Hq,Dh", [(BF16, 1, 64), (BF16, 16, 128), (BF16, 32, 64), (BF16, 40, 128), (F32, 3, 64), (F32, 2, 128)])
 @pytest.mark.parametrize("sign", [1.0, -1.0])
