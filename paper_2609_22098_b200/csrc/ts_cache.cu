@@ -179,9 +179,10 @@ __device__ int reserve_taken(const ReserveArgs& a, const long long* pre, int cou
   return top;
 }
 
-// WHERE 0: everything, by one cluster; 1: tables and slots; 2: the counts and the pages given back, by one CTA after 1
+// WHERE 0: everything, by one cluster; 1: tables and slots; 2: the counts and the pages given back, by one CTA after 1.  (One CTA an SM in
+// the bounds: the compiler takes 32 registers otherwise and spills; a round of 32 requests 5.6 and 5.4 us.)
 template <int WHERE>
-__global__ void __launch_bounds__(RES_THREADS) reserve_kernel(const ReserveArgs a) {
+__global__ void __launch_bounds__(RES_THREADS, 1) reserve_kernel(const ReserveArgs a) {
   extern __shared__ long long pre[];
   pdl_wait();
   pdl_launch_dependents();
