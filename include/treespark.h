@@ -104,7 +104,7 @@ int32_t ts_set_ablation(ts_ctx* ctx, uint32_t flags);
  *                         arrival more than will come: the waits run out, the kernels return, and the
  *                         requests are reported with TS_ERR_TIMEOUT in status[] (given parents: by NaN).  ts_tree_attention
  *                         with more than 16 query rows a kv head (bf16) expects bytes of its copies that do not come,
- *                         from the third step of a CTA on (the last, where it has fewer): the rows it then works on, and
+ *                         from the fifth step of a CTA on (the first, where it has no more than four): the rows it then works on, and
  *                         all of its later ones, are NaN */
 #define TS_TEST_FORCE_FMA 1u
 #define TS_TEST_NO_TMA 2u

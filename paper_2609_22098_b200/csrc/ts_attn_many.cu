@@ -172,6 +172,7 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
   int slot = 0, copied = 0;
   uint32_t phase = 0;
   bool alive = true;
+  uint32_t lost = half_steps > 8 ? 0u : a.lost;   // (from the fifth step on where there are more than four)
   while (copied < half_steps && alive) {
     look_up();                       // the next batch's entries are on their way while this one is copied
     const unsigned there8 = __ballot_sync(~0u, now >= 0);
@@ -181,7 +182,7 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
       if (lane == 0) {
         unsigned char* pr = &sh.present[(copied >> 1) % MANY_PRESENT];
         *pr = (unsigned char)((copied & 1) ? *pr | there << 4 : there);
-        mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * BLK + (copied >= min(4, half_steps - 1) ? a.lost : 0u));   // (from the third step on, or the last)
+        mbar_expect_tx(&sh.bars.raw_full[slot], __popc(there) * BLK + lost);
       }
       __syncwarp();
       if (lane >> 2 == k && now >= 0)
@@ -191,6 +192,7 @@ __device__ void many_load(const AttnArgs& a, ManyShared& sh, unsigned char* raw)
       if (++slot == MANY_RAW) { slot = 0; phase ^= 1u; }
     }
     now = place();
+    lost = a.lost;
   }
   // Shared memory is not given up before the last copies have come, whichever wait gives up and when (the last use of a slot completes
   // the phase before the next).
@@ -749,6 +751,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
   __syncthreads();
   tc_fence_after();
   if (sh.tmem != 0u) sh.abort = 1;   // (cannot be: 512 columns were asked for)
+  bool issuer = false;
   if (warp < MANY_SOFT) {
     many_softmax<Dh>(a, sh, smem);
   } else {
@@ -759,8 +762,7 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
     else if (warp == MANY_ISSUE) {
       if (elect_one()) {
         many_issue<Dh>(a, sh, smem);
-        mma_commit(&sh.bars.issued);   // (nor is tensor memory before the last products are complete)
-        drain(&sh.bars.issued, 0u, a.limit);
+        issuer = true;
       }
     }
     else if (warp == MANY_LOAD) many_load<Dh>(a, sh, smem + P::R);
@@ -768,6 +770,12 @@ __global__ void __launch_bounds__(MANY_THREADS, 1) attn_many_kernel(const AttnAr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  // Nor is tensor memory given up before the last products are complete.  (Without a wait that gave up the softmax warps have waited for them.)
+  if (issuer && sh.abort) {
+    mma_commit(&sh.bars.issued);
+    drain(&sh.bars.issued, 0u, a.limit);
+  }
+  __syncwarp();
   if (warp == MANY_ISSUE) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh.tmem), "r"(512u) : "memory");
 }
 

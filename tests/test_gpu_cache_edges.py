@@ -88,7 +88,7 @@ def test_queries_with_infinities_give_nan_whatever_their_scores(dtype, Hq, Dh, s
 
 @pytest.mark.parametrize("Dh,N,Hq", [(128, 1, 32), (64, 1, 24), (128, 4, 48), (64, 7, 32)])
 def test_a_wait_that_runs_out_behind_issued_products(Dh, N, Hq):
-    """The tensor-core kernel gives up in the third of some ten steps a CTA, with products of the steps before issued: it waits for them
+    """The tensor-core kernel gives up in the fifth of some ten steps a CTA, with products of the steps before issued: it waits for them
     and for its copies, its rows are NaN, and the same call without lost bytes gives what it gave before."""
     ts = context(Nmax=N, B=1)
     n = 10 * 128 * torch.cuda.get_device_properties(0).multi_processor_count
