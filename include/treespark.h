@@ -353,7 +353,9 @@ int32_t ts_calib_load_table(ts_ctx* ctx, const float* table, void* stream);
  * n_nodes[b] nodes of the request's tree and stand at positions seq_len[b] .. seq_len[b] + n_nodes[b].  A slot = page *
  * page_size + place in the page.  Row arrays are [B][Nmax+1] as ts_emit_attention_inputs lays them out; where n_nodes is
  * NULL a request has its anchor only and row arrays are [B][1] (one token per request and round).  n_nodes is clamped to
- * 0..Nmax.  seq_len[b] < 0: the request takes no part.
+ * 0..Nmax.  seq_len[b] < 0: the request takes no part.  A chunk of a prompt is a chain of rows (no mask) and has Nmax + 1 of them at
+ * most, so a longer prompt goes in chunks, or by a context of its own with Nmax = 256 (the calls of this section keep nothing in
+ * the context; one cache can serve contexts of several Nmax).
  *
  * Layout of one layer's pool, bytes: [n_pages][Hkv][page_size / 16][18 * Dh].  The 18 * Dh bytes of 16 consecutive tokens of
  * a head are K codes [16][Dh/2], V codes [2][Dh/16][8][8], K scales [16][Dh/16], V scales [2][Dh/16][8] (V: octets of
@@ -430,7 +432,8 @@ int32_t ts_tree_attention(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B,
  * seq_len[b]).
  *   ts_cache_commit_granted: the same with status DEVICE [B]: where it is not TS_OK nothing happens to the request.  Given the
  *   status of ts_cache_reserve, a request that was refused pages keeps its length; ts_cache_commit, which is not told, would count
- *   rows that were never written, and is for rounds in which no request was refused.
+ *   rows that were never written, and is for rounds in which no request was refused.  A caller whose other calls of the round have
+ *   a status too (trees, verification: after TS_ERR_TIMEOUT their outputs are not to be used) passes one that is not TS_OK wherever any is.
  */
 int32_t ts_cache_commit(ts_ctx* ctx, const ts_cache_layout* layout, int32_t B, int32_t layers, size_t layer_stride, void* pool,
                         const int32_t* block_table, const int32_t* seq_len, const int32_t* acc_len, const int32_t* acc_node,

@@ -7,10 +7,10 @@ namespace ts {
 
 // ------------------------------------------------------------------------------------------------
 // Few rows: 8 NT query rows of one kv head a unit, on mma.sync with the cache's tokens on the rows of the matrix
-// instruction (S^T = K Q^T, O^T = V^T P^T), so that one instruction of 16 x 8 serves eight query rows and no lane computes
-// for rows that are not there.  Single tokens of 64 requests of 1,000 to 16,000 tokens with eight kv heads of 128 channels (626 MB of
-// cache): 169 us, 3.7 TB/s.  The copies alone take 107 to 119 us; what is left is instruction issue, some 370 a block of 16 tokens (unpacking
-// 4,096 codes is half of them), at two a cycle of four.
+// instruction (S^T = K Q^T, O^T = V^T P^T), so that one instruction of 16 x 8 serves eight query rows (four query heads a kv head
+// leave half of its columns empty; with rows on the other side three quarters would be).  Single tokens of 64 requests of 1,000 to 16,000 tokens with eight kv heads of 128 channels (626 MB of
+// cache): 169 us, 3.7 TB/s.  The copies alone take 107 to 119 us; what is left are the fixed latencies of unpacking 4,096 codes a block of 16
+// tokens, which three warps a scheduler do not cover: 329 instructions a block, issued in 48 % of the slots.
 // ------------------------------------------------------------------------------------------------
 constexpr int FEW_WARPS = 4;
 constexpr int FEW_THREADS = FEW_WARPS * 32;
@@ -404,8 +404,8 @@ __global__ void __launch_bounds__(FEW_THREADS, F32 || NT > 1 ? 2 : 3) attn_few_k
 // ------------------------------------------------------------------------------------------------
 // Join: a CTA takes some rows of a cut unit, a warp a row; where there are many pieces, all its warps one row after the
 // other.  The pieces are added in an order that depends on their number only.  Bound by latency (the record, then sums and
-// pieces, which are loaded together): 2 us of 10 for one request of 517 tokens, 7 of 114 for 32 trees, 13 of 274 for 8
-// requests with trees of 120 to 256 nodes (up to 38 MB of pieces, from L2).
+// pieces, which are loaded together): 1.6 us of 9.8 for one request of 517 tokens, 6 of 47 for two contexts of up to
+// 131,000 (fp32), 6 of 96 for 32 trees, 14 of 235 for 8 requests with trees of 120 to 256 nodes (up to 38 MB of pieces, from L2).
 // ------------------------------------------------------------------------------------------------
 constexpr int JOIN_WARPS = 8;
 // Rows a CTA: few rows are cut into many pieces, which a CTA's warps share (1, 2, 4, 8 rows: the request 12.1, 10.3, 10.0, 10.0 us, two

@@ -10,8 +10,8 @@
 // converted keys and values; with fewer they take the same rows and every other step, and their halves are joined at the end.
 // Either way one group's exponentials run beside the other's matrix products.
 //
-// Trees of 120 to 256 nodes of 8 requests behind 2,000 to 16,000 tokens, 32 query heads on 4 of 128 channels: 236 us, 0.83 PFLOP/s, 51 % of
-// what a large matrix product reaches.  Trees of 8 to 30 nodes of 32 requests behind 500 to 6,000 tokens, 8 kv heads: 98 us, 1.3 TB/s.
+// Trees of 120 to 256 nodes of 8 requests behind 2,000 to 16,000 tokens, 32 query heads on 4 of 128 channels: 235 us on the device (join and
+// all), 0.83 PFLOP/s, 51 % of what a large matrix product reaches.  Trees of 8 to 30 nodes of 32 requests behind 500 to 6,000 tokens, 8 kv heads: 96 us, 1.3 TB/s.
 // What bounds it is the chain of a tile (scores, their largest, weights, product with V, then the next scores, which need the
 // weights' columns) and the waits between its links, which two groups cover in part; with one tile the converters (64 KB of
 // fp16 a step) are as busy.

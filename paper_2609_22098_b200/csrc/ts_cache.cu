@@ -44,7 +44,7 @@ bool on_ctx_device(const ts_ctx* ctx) {
 // cluster of eight CTAs whose barrier separates reading the counts from writing them, so that they may be updated in place;
 // where whole tables are written, many CTAs write them and a second launch updates the counts.  Bound by latency (counts, a scan, entries,
 // slots and two barriers one after the other): a round of 32 requests moves 9 KB in 5.4 us, 500 requests that start with tables of
-// up to 1,875 entries move 3.8 MB in 9.7.
+// up to 1,875 entries move 3.8 MB in 10.0.
 // ------------------------------------------------------------------------------------------------
 constexpr int RES_THREADS = 512;
 constexpr int RES_CLUSTER = 8;
@@ -291,8 +291,8 @@ static cudaError_t launch_reserve(ts_ctx* ctx, const ReserveArgs& a, cudaStream_
 // ------------------------------------------------------------------------------------------------
 // Append.  A lane takes eight elements of a row's head (two lanes share a scale), Dh/4 lanes both K and V of one (row, head),
 // so that what is not finite in either marks both.  Chunks of 64 requests (102 to 257 rows each, 4 heads of 64 channels, fp32, with
-// values): 12.6 us on the device for 50 MB, 4 TB/s; the trees of 32 requests in bf16 6.8 us for 11 MB.  Bound by issue and by the ramp of so
-// short a kernel; two rows a lane, side by side, took as long.
+// values): 12.4 us on the device for 50 MB, 4 TB/s; the trees of 32 requests in bf16 6.7 us for 11 MB.  Bound by issue (74 % of the slots while
+// SMs are active) and by the ramp of so short a kernel (they are for 71 % of it); two rows a lane, side by side, took as long.
 // ------------------------------------------------------------------------------------------------
 constexpr int APP_THREADS = 128;   // (128, 256, 512: the chunks below take 12.8, 13.1, 14.5 us in a row)
 
@@ -424,8 +424,8 @@ __global__ void __launch_bounds__(APP_THREADS) append_kernel(const AppendArgs a)
 // ------------------------------------------------------------------------------------------------
 // Commit.  A warp per (request, layer, head) holds the bytes of all moved rows before it writes one: sources and targets of
 // a path overlap.  The CTAs of a request form a cluster, whose barrier lets the new length overwrite the old.  Bound by latency
-// (nodes, table, bytes, then the writes): paths of up to eight rows of 32 requests, 12 layers of 8 heads, 8.5 us for 4 MB; of one
-// request with 36 layers 5.7 us on the device for 0.6 MB.
+// (nodes, table, bytes, then the writes): paths of up to eight rows of 32 requests, 12 layers of 8 heads, 6.4 us on the device
+// for 4 MB; of one request with 36 layers 5.8 us for 0.6 MB.
 // ------------------------------------------------------------------------------------------------
 constexpr int COM_THREADS = 1024;   // at most: a warp for each layer and head of a request
 // CTAs of a request: eight, and sixteen where a warp would have to take more than one layer and head (one request with 36 layers of
